@@ -123,6 +123,48 @@ psd_status psd_model_create_w4(const psd_model_desc *desc, const void *const *we
 size_t psd_model_packed_bytes(const psd_model *m);
 psd_status psd_model_pack(psd_model *m, void *packed_mem, size_t packed_bytes, void *hip_stream);
 
+/* ---- Rotary positions.  A psd_rope is how a model turns its query and key heads by their position: the first rot_dim of a
+ * head's d_head entries in pairs, pair i by the angle position * f_i, the others not at all.
+ *   layout   PSD_ROPE_HALF: entries (i, i + rot_dim/2) are a pair; PSD_ROPE_INTERLEAVED: (2i, 2i + 1)
+ *   scaling  with f_i = theta^(-2i/rot_dim):
+ *            PSD_ROPE_PLAIN   f_i
+ *            PSD_ROPE_LINEAR  f_i / factor: positions interpolated
+ *            PSD_ROPE_BASE    theta * factor^(rot_dim/(rot_dim-2)) in theta's place: the slowest pair slowed by factor, the fastest
+ *                             kept (rot_dim = 2: f_i)
+ *            PSD_ROPE_PARTS   by the turns a pair makes within original_len positions, n_i = original_len * f_i / (2 pi): more
+ *                             than `high`: f_i, fewer than `low`: f_i / factor, between: w f_i + (1 - w) f_i / factor with
+ *                             w = (n_i - low) / (high - low)
+ *   magnitude  cos and sin are multiplied with it (0 counts as 1)
+ * (x, y) becomes magnitude * (x cos - y sin, y cos + x sin).  Angles are reduced to a fraction of a turn in fp64.
+ * Limits: d_head even, 2 .. 256; rot_dim even, 2 .. d_head (0 counts as d_head); theta > 0; factor > 0 and 0 <= low < high,
+ * original_len > 0 where the scaling uses them; all finite.  Anything else: PSD_ERR_SHAPE. */
+#define PSD_ROPE_HALF 0
+#define PSD_ROPE_INTERLEAVED 1
+#define PSD_ROPE_PLAIN 0
+#define PSD_ROPE_LINEAR 1
+#define PSD_ROPE_BASE 2
+#define PSD_ROPE_PARTS 3
+typedef struct psd_rope psd_rope;
+typedef struct {
+    int32_t d_head, rot_dim, layout, scaling;
+    float theta, factor, low, high;
+    int32_t original_len;
+    float magnitude;
+} psd_rope_desc;
+psd_status psd_rope_create(const psd_rope_desc *desc, psd_rope **out);
+psd_status psd_rope_destroy(psd_rope *rope);
+/* The rot_dim/2 frequencies f_i (radians a position) into a HOST array. */
+psd_status psd_rope_frequencies(const psd_rope *rope, double *out_host);
+/* Turns the heads of `rows` rows: x, y device [rows][n_heads][d_head] of `dtype`, rows x_row_stride / y_row_stride elements
+ * apart, heads dense; positions device int32[rows].  y may be x (the strides then equal); otherwise no element of y may be one of x.
+ * Query and key heads that lie side by side in a row are one call.  rows = 0 is a no-op. */
+psd_status psd_rope_rotate(const psd_rope *rope, const void *x, void *y, const int32_t *positions, int32_t rows, int32_t n_heads,
+                           int32_t dtype, int64_t x_row_stride, int64_t y_row_stride, void *hip_stream);
+/* Forwards of m turn by `rope` (copied; NULL: by the descriptor's rope_theta again) instead.  Its d_head must be the model's.
+ * Call it before sizing workspaces.  psd_model_forward_tree needs PSD_ROPE_HALF over the whole head (PSD_ERR_UNIMPLEMENTED
+ * otherwise). */
+psd_status psd_model_set_rope(psd_model *m, const psd_rope *rope);
+
 /* Bytes of workspace psd_model_forward needs for this batch / n_new / cache length
  * (0 on a bad argument).  The workspace must be 256-byte aligned. */
 size_t psd_model_workspace_bytes(const psd_model *m, int32_t batch, int32_t n_new, int32_t max_len);
@@ -139,6 +181,58 @@ size_t psd_kv_bytes(const psd_model *m, int32_t batch, int32_t max_len);
 psd_status psd_kv_create(const psd_model *m, int32_t batch, int32_t max_len, void *k_mem,
                          void *v_mem, int32_t *lens_dev, int32_t len_upper_bound, psd_kv **out);
 psd_status psd_kv_destroy(psd_kv *kv);
+/* ---- A KV cache in 8 bits: e4m3 codes (as OCP FP8: 4 exponent, 3 mantissa bits, largest value 448, no infinities), and one fp32
+ * scale for every 64 tokens of a KV head, of K and of V apart.  An entry stands for code * scale.
+ *   k_codes [n_layers][batch][n_kv_heads][max_len][d_head]
+ *   v_codes [n_layers][batch][n_kv_heads][max_len/64][d_head][64]    (each block of 64 tokens transposed)
+ *   k_scale, v_scale  fp32 [n_layers][batch][n_kv_heads][max_len/64]
+ * Codes: psd_kv_q8_bytes() bytes each, scales: psd_kv_q8_scale_bytes() each, all 256-byte aligned.
+ * A psd_kv of this kind goes wherever one of psd_kv_create goes, with the same meaning, but for token trees
+ * (psd_model_forward_tree, psd_kv_compact_tree: PSD_ERR_UNIMPLEMENTED).  PSD_BF16 models only (PSD_ERR_DTYPE; sizes 0).  The rows of
+ * a step are read back in 8 bits too, by the step itself. */
+size_t psd_kv_q8_bytes(const psd_model *m, int32_t batch, int32_t max_len);
+size_t psd_kv_q8_scale_bytes(const psd_model *m, int32_t batch, int32_t max_len);
+psd_status psd_kv_create_q8(const psd_model *m, int32_t batch, int32_t max_len, void *k_codes, void *v_codes, float *k_scale,
+                            float *v_scale, int32_t *lens_dev, int32_t len_upper_bound, psd_kv **out);
+
+/* The two steps of a forward pass that touch such a cache, on one layer of it, for programs with projections of their own. */
+typedef struct {
+    void *k_codes, *v_codes;          /* device, one layer of the layouts above, 16-byte aligned */
+    float *k_scale, *v_scale;
+    const int32_t *lens;              /* device int32[batch]: valid positions before the step */
+    int32_t batch, n_kv_heads, d_head, max_len;      /* d_head 64 or 128; max_len a multiple of 64 */
+} psd_kv8_view;
+/* *out <- layer `layer` of an 8-bit psd_kv (PSD_ERR_DTYPE: it is not one). */
+psd_status psd_kv8_layer(const psd_kv *kv, int32_t layer, psd_kv8_view *out);
+/* Rotates, quantises and appends the n_new new rows of every sequence: row b * n_new + r sits at position lens[b] + r.
+ *   rope      how query and key heads turn; NULL: they do not
+ *   q, k, v   device, `dtype`, rows *_row_stride elements apart, heads dense within a row (pointers into one buffer of
+ *             projections are fine); q [..][n_q_heads][d_head] or NULL, k and v [..][n_kv_heads][d_head]
+ *   q_out     the rotated queries, same type; NULL iff q is; may be q itself (with its stride)
+ * For each block of 64 tokens and KV head, of K and V apart: scale = the smallest power of two, between 2^-40 and 2^40, with
+ * max |x| <= 448 scale over the finite entries written, or the block's present scale if that is larger and older tokens
+ * (positions below lens[b]) lie in the block; code = x / scale rounded to nearest even (finite entries beyond 448 scale to 448, infinities
+ * and NaN to NaN); where the scale grew, the older tokens' codes are divided by the ratio and rounded likewise.  Positions
+ * outside lens[b] .. lens[b]+n_new-1 are otherwise left as they are, and lens too: the caller moves it on after
+ * psd_kv8_attention.  Rows at or beyond max_len are not written.  len_upper_bound: the caller's bound of lens[b] + n_new
+ * (PSD_ERR_CAPACITY if it is beyond max_len). */
+psd_status psd_kv8_append(const psd_kv8_view *cache, const psd_rope *rope, const void *q, const void *k, const void *v, void *q_out,
+                          int32_t n_new, int32_t n_q_heads, int32_t dtype, int64_t q_row_stride, int64_t k_row_stride,
+                          int64_t v_row_stride, int64_t q_out_row_stride, int32_t len_upper_bound, void *hip_stream);
+/* out = softmax(scale * q K^T) V for the rows just appended: row r of sequence b sees positions 0 .. lens[b] + r (lens as
+ * before the step).  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   q, out    device bf16 [batch * n_new][n_q_heads][d_head], rows *_row_stride elements apart, both 16-byte aligned with strides
+ *             a multiple of 8 (PSD_ERR_SHAPE); out may not overlap q
+ *   scale     0: 1 / sqrt(d_head)
+ *   workspace 256-byte aligned, psd_kv8_attention_workspace_bytes() of the same numbers (0 bytes: may be NULL)
+ * Scales in the cache must be positive, finite and between 2^-40 and 2^40.  What lies at positions that a row does not
+ * see has no part in its result, whatever it is.  Sums, softmax and outputs in fp32, weights rounded to fp16. */
+size_t psd_kv8_attention_workspace_bytes(int32_t batch, int32_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t d_head,
+                                         int32_t len_upper_bound);
+psd_status psd_kv8_attention(const psd_kv8_view *cache, const void *q, void *out, int32_t n_new, int32_t n_q_heads, float scale,
+                             int64_t q_row_stride, int64_t out_row_stride, int32_t len_upper_bound, void *workspace, size_t ws_bytes,
+                             void *hip_stream);
+
 /* The host-side upper bound of lens (for tests and capacity planning). */
 int32_t psd_kv_len_upper_bound(const psd_kv *kv);
 
@@ -292,7 +386,7 @@ psd_status psd_kv_compact_tree(psd_kv *kv, const int32_t *base_lens_dev, const i
 #define PSD_KIND_GEMM_SKINNY 3       /* bf16 weight-streaming GEMM over packed 16 KB units, M <= 16: by 16 KB units, or QKV and gate|up by bands (gate|up with SwiGLU; heads in whole tiles with their epilogue) */
 #define PSD_KIND_GEMM_TILED 4        /* GEMM of bf16 models with fp16 MFMA, M > 16: LDS-tiled, or (packed, M <= 128) on streamed units */
 #define PSD_KIND_GEMM_REDUCE 5       /* split-K reduction */
-#define PSD_KIND_ROPE_APPEND 6
+#define PSD_KIND_ROPE_APPEND 6       /* rotation and append, in the cache's type */
 #define PSD_KIND_ATTN 7
 #define PSD_KIND_ATTN_COMBINE 8
 #define PSD_KIND_SWIGLU 9
@@ -303,7 +397,8 @@ psd_status psd_kv_compact_tree(psd_kv *kv, const int32_t *base_lens_dev, const i
 #define PSD_KIND_GEMM_COLUMN 14      /* bf16 GEMM with the residual epilogue (O, down), M <= 16 */
 #define PSD_KIND_GEMM_W4 15          /* 4-bit weight-only GEMM, M <= 16 */
 #define PSD_KIND_GEMM_SLOT 16        /* bf16 GEMM on 16-column tiles x K splits, M <= 16 (one partial slot, or unpacked weights) */
-#define PSD_KIND_COUNT 17
+#define PSD_KIND_ROPE 17             /* rotary positions by themselves: psd_rope_rotate, a forward's table for psd_model_set_rope */
+#define PSD_KIND_COUNT 18
 psd_status psd_profile_enable(int32_t max_launches);
 psd_status psd_profile_collect(double *ms_by_kind, int64_t *launches_by_kind);
 

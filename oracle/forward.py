@@ -81,6 +81,12 @@ class KVCache:
         self.lens = np.zeros(batch, np.int64)
         self.max_len = max_len
 
+    def append(self, l, b, s0, k, v):
+        """The new rows k, v [R, h_kv, d_h] of sequence b in layer l, from position s0 on."""
+        R = k.shape[0]
+        self.k[l][b, :, s0:s0 + R] = k.transpose(1, 0, 2)
+        self.v[l][b, :, s0:s0 + R] = v.transpose(1, 0, 2)
+
     def truncate(self, new_lens):
         """Rollback to the accepted length (the 'partial rollback' of Sec. 3.3): only the
         length changes, stale rows are overwritten by the next append."""
@@ -110,10 +116,12 @@ def attention(q, k, v, n_past):
     return out
 
 
-def forward(cfg: ModelConfig, weights: dict, tokens, kv: KVCache):
+def forward(cfg: ModelConfig, weights: dict, tokens, kv: KVCache, turn=None):
     """One forward pass over tokens [B, R] appended at positions lens[b]..lens[b]+R-1.
     Appends their K/V, advances lens by R and returns fp64 logits [B, R, V]; row r is the
-    distribution of the token that follows input token r."""
+    distribution of the token that follows input token r.  turn(x, positions): the model's rotary
+    positions where they are not rope's (rotary.py)."""
+    turn = turn or (lambda x, positions: rope(x, positions, cfg.rope_theta))
     tokens = np.asarray(tokens)
     B, R = tokens.shape
     if np.any(kv.lens + R > kv.max_len):
@@ -130,10 +138,9 @@ def forward(cfg: ModelConfig, weights: dict, tokens, kv: KVCache):
         for b in range(B):
             s0 = int(kv.lens[b])
             pos = np.arange(s0, s0 + R)
-            qb = rope(q[b], pos, cfg.rope_theta)
-            kb = rope(k[b], pos, cfg.rope_theta)
-            kv.k[l][b, :, s0:s0 + R] = kb.transpose(1, 0, 2)
-            kv.v[l][b, :, s0:s0 + R] = v[b].transpose(1, 0, 2)
+            qb = turn(q[b], pos)
+            kb = turn(k[b], pos)
+            kv.append(l, b, s0, kb, v[b])
             a[b] = attention(qb, widen(kv.k[l][b, :, :s0 + R]), widen(kv.v[l][b, :, :s0 + R]), s0)
         x = x + a.reshape(B, R, h_q * d_h) @ w("wo").T
         n = rmsnorm(x, w("ffn_norm"), cfg.rms_eps)

@@ -15,6 +15,8 @@ PSD_ERR_TEMPERATURE, PSD_ERR_WORKSPACE, PSD_ERR_HIP, PSD_ERR_UNIMPLEMENTED = -5,
 PSD_F32, PSD_BF16 = 0, 1
 PSD_FLAG_NEAR_TIE, PSD_FLAG_ZERO_RESIDUAL = 1, 2
 PSD_STATIC_SCRATCH_BYTES = 1 << 20
+PSD_ROPE_HALF, PSD_ROPE_INTERLEAVED = 0, 1
+PSD_ROPE_PLAIN, PSD_ROPE_LINEAR, PSD_ROPE_BASE, PSD_ROPE_PARTS = 0, 1, 2, 3
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpsd.so")
@@ -29,6 +31,16 @@ class psd_model_desc(ctypes.Structure):
                 ("rms_eps", _f32), ("dtype", _i32)]
 
 
+class psd_rope_desc(ctypes.Structure):
+    _fields_ = [("d_head", _i32), ("rot_dim", _i32), ("layout", _i32), ("scaling", _i32), ("theta", _f32), ("factor", _f32),
+                ("low", _f32), ("high", _f32), ("original_len", _i32), ("magnitude", _f32)]
+
+
+class psd_kv8_view(ctypes.Structure):
+    _fields_ = [("k_codes", _vp), ("v_codes", _vp), ("k_scale", _vp), ("v_scale", _vp), ("lens", _vp), ("batch", _i32),
+                ("n_kv_heads", _i32), ("d_head", _i32), ("max_len", _i32)]
+
+
 _SIGNATURES = {
     "psd_status_string": (ctypes.c_char_p, [_i32]),
     "psd_last_hip_error": (_i32, []),
@@ -41,6 +53,19 @@ _SIGNATURES = {
     "psd_model_pack": (_i32, [_vp, _vp, _sz, _vp]),
     "psd_kv_bytes": (_sz, [_vp, _i32, _i32]),
     "psd_kv_create": (_i32, [_vp, _i32, _i32, _vp, _vp, _vp, _i32, ctypes.POINTER(_vp)]),
+    "psd_rope_create": (_i32, [ctypes.POINTER(psd_rope_desc), ctypes.POINTER(_vp)]),
+    "psd_rope_destroy": (_i32, [_vp]),
+    "psd_rope_frequencies": (_i32, [_vp, ctypes.POINTER(ctypes.c_double)]),
+    "psd_rope_rotate": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _i64, _i64, _vp]),
+    "psd_model_set_rope": (_i32, [_vp, _vp]),
+    "psd_kv_q8_bytes": (_sz, [_vp, _i32, _i32]),
+    "psd_kv_q8_scale_bytes": (_sz, [_vp, _i32, _i32]),
+    "psd_kv_create_q8": (_i32, [_vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _i32, ctypes.POINTER(_vp)]),
+    "psd_kv8_layer": (_i32, [_vp, _i32, ctypes.POINTER(psd_kv8_view)]),
+    "psd_kv8_append": (_i32, [ctypes.POINTER(psd_kv8_view), _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i64, _i64, _i64, _i64,
+                              _i32, _vp]),
+    "psd_kv8_attention_workspace_bytes": (_sz, [_i32, _i32, _i32, _i32, _i32, _i32]),
+    "psd_kv8_attention": (_i32, [ctypes.POINTER(psd_kv8_view), _vp, _vp, _i32, _i32, _f32, _i64, _i64, _i32, _vp, _sz, _vp]),
     "psd_kv_destroy": (_i32, [_vp]),
     "psd_kv_len_upper_bound": (_i32, [_vp]),
     "psd_model_forward": (_i32, [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _sz, _vp]),
@@ -62,7 +87,7 @@ _SIGNATURES = {
 
 PSD_KIND_NAMES = ("embed", "rmsnorm", "gemm_f32", "gemm_skinny", "gemm_tiled", "gemm_reduce", "rope_append", "attn",
                   "attn_combine", "swiglu", "lens", "accept_stats", "accept_draw", "accept_locate", "gemm_column", "gemm_w4",
-                  "gemm_slot")
+                  "gemm_slot", "rope")
 
 _lib = None
 
@@ -164,6 +189,49 @@ def psd_kv_create(model, batch, max_len, k_mem, v_mem, lens_dev, len_upper_bound
     return out
 
 
+def psd_rope_create(desc: psd_rope_desc):
+    out = _vp()
+    _check(lib().psd_rope_create(ctypes.byref(desc), ctypes.byref(out)), "psd_rope_create")
+    return out
+
+
+def psd_rope_destroy(rope):
+    _check(lib().psd_rope_destroy(rope), "psd_rope_destroy")
+
+
+def psd_rope_frequencies(rope, n):
+    """-> the n = rot_dim / 2 frequencies, a list of floats."""
+    out = (ctypes.c_double * n)()
+    _check(lib().psd_rope_frequencies(rope, out), "psd_rope_frequencies")
+    return list(out)
+
+
+def psd_model_set_rope(model, rope):
+    _check(lib().psd_model_set_rope(model, rope), "psd_model_set_rope")
+
+
+def psd_kv_q8_bytes(model, batch, max_len):
+    return lib().psd_kv_q8_bytes(model, batch, max_len)
+
+
+def psd_kv_q8_scale_bytes(model, batch, max_len):
+    return lib().psd_kv_q8_scale_bytes(model, batch, max_len)
+
+
+def psd_kv_create_q8(model, batch, max_len, k_codes, v_codes, k_scale, v_scale, lens_dev, len_upper_bound):
+    out = _vp()
+    _check(lib().psd_kv_create_q8(model, batch, max_len, _ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale), _ptr(lens_dev),
+                                  len_upper_bound, ctypes.byref(out)), "psd_kv_create_q8")
+    return out
+
+
+def psd_kv8_layer(kv, layer):
+    """-> the psd_kv8_view of one layer of an 8-bit cache."""
+    out = psd_kv8_view()
+    _check(lib().psd_kv8_layer(kv, layer, ctypes.byref(out)), "psd_kv8_layer")
+    return out
+
+
 def psd_kv_destroy(kv):
     _check(lib().psd_kv_destroy(kv), "psd_kv_destroy")
 
@@ -177,6 +245,30 @@ def psd_model_forward(model, tokens_dev, n_new, kv, logits_out_dev, n_logit_rows
     _check(lib().psd_model_forward(model, _ptr(tokens_dev), n_new, kv, _ptr(logits_out_dev), n_logit_rows,
                                    _ptr(workspace), workspace.numel() * workspace.element_size(),
                                    _stream_ptr(stream)), "psd_model_forward")
+
+
+def psd_rope_rotate(rope, x, y, positions, rows, n_heads, dtype, x_row_stride, y_row_stride, stream=None):
+    _check(lib().psd_rope_rotate(rope, _ptr(x), _ptr(y), _ptr(positions), rows, n_heads, dtype, x_row_stride, y_row_stride,
+                                 _stream_ptr(stream)), "psd_rope_rotate")
+
+
+def psd_kv8_append(cache: psd_kv8_view, rope, q, k, v, q_out, n_new, n_q_heads, dtype, q_row_stride, k_row_stride, v_row_stride,
+                   q_out_row_stride, len_upper_bound, stream=None):
+    _check(lib().psd_kv8_append(ctypes.byref(cache), rope, _ptr(q), _ptr(k), _ptr(v), _ptr(q_out), n_new, n_q_heads, dtype,
+                                q_row_stride, k_row_stride, v_row_stride, q_out_row_stride, len_upper_bound, _stream_ptr(stream)),
+           "psd_kv8_append")
+
+
+def psd_kv8_attention_workspace_bytes(batch, n_new, n_q_heads, n_kv_heads, d_head, len_upper_bound):
+    return lib().psd_kv8_attention_workspace_bytes(batch, n_new, n_q_heads, n_kv_heads, d_head, len_upper_bound)
+
+
+def psd_kv8_attention(cache: psd_kv8_view, q, out, n_new, n_q_heads, scale, q_row_stride, out_row_stride, len_upper_bound, workspace,
+                      stream=None):
+    _check(lib().psd_kv8_attention(ctypes.byref(cache), _ptr(q), _ptr(out), n_new, n_q_heads, float(scale), q_row_stride,
+                                   out_row_stride, len_upper_bound, _ptr(workspace),
+                                   0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+           "psd_kv8_attention")
 
 
 def psd_spec_accept_workspace_bytes(rows, gamma, n_p_rows, vocab):

@@ -25,11 +25,13 @@ from paper_2510_26527_amd import runtime
 
 
 class Level:
-    """One model of the chain with its batch-1 KV cache and logits row buffer."""
+    """One model of the chain with its batch-1 KV cache (kv_bits 8: e4m3 codes, 16: the model's type) and logits row buffer."""
 
-    def __init__(self, model: runtime.Model, max_len: int, max_rows: int):
+    def __init__(self, model: runtime.Model, max_len: int, max_rows: int, kv_bits: int = 16):
+        if kv_bits not in (8, 16):
+            raise ValueError("kv_bits is 8 or 16")
         self.model = model
-        self.kv = runtime.KVCache(model, 1, max_len)
+        self.kv = (runtime.KVCache8 if kv_bits == 8 else runtime.KVCache)(model, 1, max_len)
         self.kv_len = 0
         self.rows = torch.empty((max_rows, model.shape.vocab), dtype=torch.float32, device=model.device)
         self.max_rows = max_rows

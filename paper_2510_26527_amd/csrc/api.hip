@@ -34,8 +34,20 @@ bool prof_acquire(hipEvent_t *start, hipEvent_t *stop) {
 }
 }  // namespace psd
 
+struct psd_rope {
+    int d_head;
+    RopeParams p;
+    RopeTurns turns;
+    double freq[kRopeMaxHead / 2];
+    // pairs (i, i + d_head / 2) of the whole head, as kernels that know no other take them
+    bool whole_half() const { return !p.interleaved && p.rot == d_head; }
+};
+
 struct psd_model {
     psd_model_desc d;
+    bool has_rope = false;           // psd_model_set_rope
+    psd_rope rope;
+    const RopeParams *pairs() const { return has_rope && !rope.whole_half() ? &rope.p : nullptr; }
     std::vector<const void *> w;     // the caller's weight pointers, in header order
     const void *embed() const { return w[0]; }
     const void *layer(int l, int which) const { return w[1 + 9 * l + which]; }
@@ -62,6 +74,8 @@ struct psd_kv {
     void *k, *v;
     int32_t *lens;
     int len_ub;                      // host upper bound of every lens[b]
+    bool q8 = false;                 // psd_kv_create_q8: k and v are codes, and these their scales
+    float *k_scale = nullptr, *v_scale = nullptr;
 };
 
 static thread_local int32_t g_last_hip_error = 0;
@@ -249,6 +263,27 @@ psd_status psd_kv_create(const psd_model *m, int32_t batch, int32_t max_len, voi
     return PSD_OK;
 }
 
+size_t psd_kv_q8_bytes(const psd_model *m, int32_t batch, int32_t max_len) {
+    if (!m || m->d.dtype != PSD_BF16 || batch <= 0 || max_len <= 0 || max_len % kKv8Block) return 0;
+    return (size_t)m->d.n_layers * batch * m->d.n_kv_heads * max_len * m->d.d_head;
+}
+size_t psd_kv_q8_scale_bytes(const psd_model *m, int32_t batch, int32_t max_len) {
+    if (!m || m->d.dtype != PSD_BF16 || batch <= 0 || max_len <= 0 || max_len % kKv8Block) return 0;
+    return (size_t)m->d.n_layers * batch * m->d.n_kv_heads * (max_len / kKv8Block) * sizeof(float);
+}
+psd_status psd_kv_create_q8(const psd_model *m, int32_t batch, int32_t max_len, void *k_codes, void *v_codes, float *k_scale,
+                            float *v_scale, int32_t *lens_dev, int32_t len_upper_bound, psd_kv **out) {
+    if (!m || !k_scale || !v_scale) return PSD_ERR_NULL;
+    if (m->d.dtype != PSD_BF16) return PSD_ERR_DTYPE;
+    if ((uintptr_t)k_scale % 256 || (uintptr_t)v_scale % 256) return PSD_ERR_SHAPE;
+    psd_kv *kv = nullptr;
+    const psd_status s = psd_kv_create(m, batch, max_len, k_codes, v_codes, lens_dev, len_upper_bound, out ? &kv : nullptr);
+    if (s != PSD_OK) return s;
+    kv->q8 = true; kv->k_scale = k_scale; kv->v_scale = v_scale;
+    *out = kv;
+    return PSD_OK;
+}
+
 psd_status psd_kv_destroy(psd_kv *kv) {
     if (!kv) return PSD_ERR_NULL;
     delete kv;
@@ -264,7 +299,7 @@ namespace {
 
 struct ForwardPlan {
     int M, width_qkv;
-    int sk_qkv, sk_o, sk_gu, sk_down, sk_head, attn_splits;
+    int sk_qkv, sk_o, sk_gu, sk_down, sk_head, attn_splits, attn_range;
     size_t off_x, off_xn, off_q, off_attn, off_h, off_partial, off_po, off_pml, off_sumsq, off_rope, off_tilectr, off_tree, total;
     size_t off_xn16, off_attn16, off_h16;
     bool half_copies;             // bf16, M > kStreamMaxRows or 4-bit projections: the producers also leave fp16 copies of the activations
@@ -332,15 +367,20 @@ size_t head_partial_bytes(const psd_model *mdl, int Ml, bool folded, int *slots)
 }
 
 // ... and the rest: attention splits, where everything lies in the workspace
-void plan_layout(const psd_model *mdl, int batch, int n_new, int len_bound, bool tree, size_t head_bytes, ForwardPlan *out,
+void plan_layout(const psd_model *mdl, int batch, int n_new, int len_bound, bool tree, bool q8, size_t head_bytes, ForwardPlan *out,
                  bool any_len = false) {
     const psd_model_desc &d = mdl->d;
     ForwardPlan &p = *out;
     const int M = p.M, hd = d.n_q_heads * d.d_head;
     const int n_o[1] = {d.d_model};
-    p.fused_rope = attn_fuses_rope(d.dtype, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, tree);
-    p.attn_splits = (any_len ? attn_max_splits : attn_pick_splits)(d.dtype, batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head,
-                                                                   len_bound, tree);
+    p.fused_rope = !q8 && !mdl->pairs() && attn_fuses_rope(d.dtype, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, tree);
+    p.attn_range = 0;
+    if (q8)
+        p.attn_splits = any_len ? kv8_attn_max_splits(batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, len_bound)
+                                : kv8_attn_splits(batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, len_bound, &p.attn_range);
+    else
+        p.attn_splits = (any_len ? attn_max_splits : attn_pick_splits)(d.dtype, batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head,
+                                                                       len_bound, tree);
     const size_t act = 4;                                    // activations are fp32 for both dtypes
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += align256(bytes); return o; };
@@ -357,15 +397,15 @@ void plan_layout(const psd_model *mdl, int batch, int n_new, int len_bound, bool
     p.off_po = take(p.attn_splits > 1 ? (size_t)M * d.n_q_heads * p.attn_splits * d.d_head * 4 : 0);
     p.off_pml = take(p.attn_splits > 1 ? (size_t)M * d.n_q_heads * p.attn_splits * 2 * 4 : 0);
     p.off_sumsq = take(p.folded ? (size_t)(d.d_model / 16) * M * 4 : 0);
-    p.off_rope = take(d.dtype == PSD_BF16 ? (size_t)M * (d.d_head / 2) * sizeof(float2) : 0);
+    p.off_rope = take(d.dtype == PSD_BF16 || mdl->has_rope ? (size_t)M * (d.d_head / 2) * sizeof(float2) : 0);
     p.off_tilectr = take(p.o_by_units || p.down_by_units ? (size_t)gemm_pack_tiles(n_o, 1) * 4 : 0);       // arrival counters
     p.off_tree = take(p.fused_rope ? (size_t)kTreeMaxNodes * 4 : 0);      // ancestor masks of a tree pass
     p.total = off;
 }
 
-ForwardPlan plan_forward(const psd_model *mdl, int batch, int n_new, int n_logit_rows, int len_bound, bool tree) {
+ForwardPlan plan_forward(const psd_model *mdl, int batch, int n_new, int n_logit_rows, int len_bound, bool tree, bool q8) {
     ForwardPlan p = plan_projections(mdl, batch * n_new);
-    plan_layout(mdl, batch, n_new, len_bound, tree, head_partial_bytes(mdl, batch * n_logit_rows, p.folded, &p.sk_head), &p);
+    plan_layout(mdl, batch, n_new, len_bound, tree, q8, head_partial_bytes(mdl, batch * n_logit_rows, p.folded, &p.sk_head), &p);
     return p;
 }
 
@@ -413,8 +453,9 @@ size_t psd_model_workspace_bytes(const psd_model *m, int32_t batch, int32_t n_ne
     ForwardPlan p = plan_projections(m, batch * n_new);
     const size_t head = worst_head_partial_bytes(m, batch, n_new, p.folded);
     size_t worst = 0;
-    for (int tree = 0; tree < 2; ++tree) {
-        plan_layout(m, batch, n_new, max_len, tree != 0, head, &p, true);
+    for (int kind = 0; kind < 3; ++kind) {               // rows, a token tree, rows on an 8-bit cache
+        if (kind == 2 && m->d.dtype != PSD_BF16) continue;
+        plan_layout(m, batch, n_new, max_len, kind == 1, kind == 2, head, &p, true);
         worst = p.total > worst ? p.total : worst;
     }
     return worst;
@@ -444,7 +485,7 @@ static psd_status forward_once(psd_model *m, const int32_t *tokens_dev, int32_t 
     const psd_model_desc &d = m->d;
     const int B = kv->batch;
     const int len_bound = kv->len_ub + n_new;
-    const ForwardPlan p = plan_forward(m, B, n_new, n_logit_rows, len_bound, tree != nullptr);
+    const ForwardPlan p = plan_forward(m, B, n_new, n_logit_rows, len_bound, tree != nullptr, kv->q8);
     if (!workspace || (uintptr_t)workspace % 256 || ws_bytes < p.total) return PSD_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)hip_stream;
     char *ws = (char *)workspace;
@@ -458,7 +499,8 @@ static psd_status forward_once(psd_model *m, const int32_t *tokens_dev, int32_t 
     uint16_t *h16 = p.half_copies ? (uint16_t *)(ws + p.off_h16) : nullptr;
     float *partial = (float *)(ws + p.off_partial);
     const int M = p.M, hd = d.n_q_heads * d.d_head, kvd = d.n_kv_heads * d.d_head;
-    const size_t kv_layer = (size_t)B * d.n_kv_heads * kv->max_len * d.d_head * elem_size(d.dtype);
+    const size_t kv_layer = (size_t)B * d.n_kv_heads * kv->max_len * d.d_head * (kv->q8 ? 1 : elem_size(d.dtype));
+    const size_t scale_layer = (size_t)B * d.n_kv_heads * (kv->max_len / kKv8Block);
 
     (void)hipGetLastError();
     auto norm_gain = [&](int l) { return l < d.n_layers ? m->layer(l, W_ATTN_NORM) : m->final_norm(); };
@@ -523,7 +565,8 @@ static psd_status forward_once(psd_model *m, const int32_t *tokens_dev, int32_t 
         }
     };
     RopeTable rt{};
-    if (d.dtype == PSD_BF16) rt = RopeTable{(float2 *)(ws + p.off_rope), kv->lens, n_new, d.d_head, d.rope_theta};
+    float2 *cs = d.dtype == PSD_BF16 || m->has_rope ? (float2 *)(ws + p.off_rope) : nullptr;        // the rows' (cos, sin)
+    if (cs && !m->has_rope) rt = RopeTable{cs, kv->lens, n_new, d.d_head, d.rope_theta};
     const uint32_t *tree_anc = nullptr;
     if (tree) {
         // a token tree: positions by depth, visibility by ancestry (both only exist in the fused attention build)
@@ -536,24 +579,42 @@ static psd_status forward_once(psd_model *m, const int32_t *tokens_dev, int32_t 
     launch_embed_norm(d.dtype, m->embed(), tokens_dev, x, norm_gain(0), p.folded || first_rows.op ? nullptr : xn, p.folded ? sumsq : nullptr, M, d.d_model,
                       d.vocab, d.rms_eps, rt, xn16, first_rows, ZeroFill{tile_ctr, arrivals ? gemm_pack_tiles(n_o_fw, 1) : 0},
                       tree, tree ? (uint32_t *)(ws + p.off_tree) : nullptr, st);
+    if (m->has_rope) launch_rope_table(cs, d.d_head / 2, kv->lens, M, n_new, m->rope.p, m->rope.turns, tree, st);
     rs.tiles = 1;
     for (int l = 0; l < d.n_layers; ++l) {
         gemm(act, M, d.d_model, m->layer(l, W_Q), hd, m->layer(l, W_K), kvd, m->layer(l, W_V), kvd, p.sk_qkv, partial,
              m->pack(l, P_QKV), l, 0);
         const RowScale qkv_rs = p.qkv_scaled ? RowScale{} : rs;           // for whoever reads the partial sums
         char *kl = (char *)kv->k + (size_t)l * kv_layer, *vl = (char *)kv->v + (size_t)l * kv_layer;
-        if (!p.fused_rope)
+        if (kv->q8) {
+            Kv8AppendArgs ap{};
+            ap.k_codes = (uint8_t *)kl; ap.v_codes = (uint8_t *)vl;
+            ap.k_scale = kv->k_scale + l * scale_layer; ap.v_scale = kv->v_scale + l * scale_layer;
+            ap.lens = kv->lens; ap.q_out = q; ap.q_out_stride = hd;
+            ap.B = B; ap.R = n_new; ap.h_q = d.n_q_heads; ap.h_kv = d.n_kv_heads; ap.d_h = d.d_head; ap.max_len = kv->max_len;
+            ap.rope = m->has_rope ? m->rope.p : RopeParams{d.d_head, 0, 1.0f};
+            ap.cs = cs; ap.cs_stride = d.d_head / 2; ap.rs = qkv_rs;
+            launch_kv8_append(ap, Kv8Source{partial, partial + hd, partial + hd + kvd, p.width_qkv, p.width_qkv, p.width_qkv, false, p.sk_qkv, (int64_t)M * p.width_qkv}, st);
+            Kv8AttnArgs at{};
+            at.q = q; at.q_stride = hd; at.k = (const uint8_t *)kl; at.v = (const uint8_t *)vl; at.k_scale = ap.k_scale; at.v_scale = ap.v_scale;
+            at.lens = kv->lens; at.B = B; at.R = n_new; at.h_q = d.n_q_heads; at.h_kv = d.n_kv_heads; at.d_h = d.d_head; at.max_len = kv->max_len;
+            at.scale = 1.0f / sqrtf((float)d.d_head); at.splits = p.attn_splits; at.range = p.attn_range;
+            at.out16 = attn16;
+            if (!p.half_copies) { if (p.folded) at.out_op = (uint16_t *)attn; else at.out = attn; }
+            at.op_folded = op_folded; at.part_o = (float *)(ws + p.off_po); at.part_ml = (float2 *)(ws + p.off_pml);
+            launch_kv8_attention(at, st);
+        } else if (!p.fused_rope)
             launch_reduce_rope_append(d.dtype, partial, p.sk_qkv, qkv_rs, q, kl, vl, kv->lens, B, n_new, d.n_q_heads,
-                                      d.n_kv_heads, d.d_head, kv->max_len, d.rope_theta, rt.cs, st);
+                                      d.n_kv_heads, d.d_head, kv->max_len, d.rope_theta, cs, m->pairs(), st);
         AttnArgs a{};
-        if (p.fused_rope) { a.qkv_partial = partial; a.qkv_splits = p.sk_qkv; a.rs = qkv_rs; a.rope_cs = rt.cs; a.tree_anc = tree_anc; }
+        if (p.fused_rope) { a.qkv_partial = partial; a.qkv_splits = p.sk_qkv; a.rs = qkv_rs; a.rope_cs = cs; a.tree_anc = tree_anc; }
         a.q = q; a.k = kl; a.v = vl; a.lens = kv->lens; a.out16 = attn16;        // the O projection reads one of the three
         if (!p.half_copies) { if (p.folded) a.out_op = (uint16_t *)attn; else a.out = attn; }
         a.op_folded = op_folded;
         a.B = B; a.R = n_new; a.h_q = d.n_q_heads; a.h_kv = d.n_kv_heads; a.d_h = d.d_head; a.max_len = kv->max_len;
         a.len_bound = len_bound; a.part_o = (float *)(ws + p.off_po); a.part_ml = (float *)(ws + p.off_pml);
         a.splits = p.attn_splits;
-        launch_attention(d.dtype, a, st);
+        if (!kv->q8) launch_attention(d.dtype, a, st);
 
         resid_gemm(attn, hd, m->layer(l, W_O), p.sk_o, m->pack(l, P_O), m->layer(l, W_FFN_NORM), p.o_by_units, l, 3);
         gemm(act, M, d.d_model, m->layer(l, W_GATE), d.d_ffn, m->layer(l, W_UP), d.d_ffn, nullptr, 0, p.sk_gu,
@@ -716,6 +777,7 @@ psd_status psd_model_forward_tree(psd_model *m, const int32_t *tokens_dev, int32
     const int B = kv->batch;
     TreeShape ts{};
     if (!forward_shape_ok(m, B, n_nodes) || !tree_shape_from_parents(parents_host, n_nodes, kTreeMaxNodes, &ts)) return PSD_ERR_SHAPE;
+    if (kv->q8) return PSD_ERR_UNIMPLEMENTED;
     if (kv->len_ub + n_nodes > kv->max_len) return PSD_ERR_CAPACITY;
     if (m->w4 && !m->packed) return PSD_ERR_UNIMPLEMENTED;
     return forward_once(m, tokens_dev, n_nodes, kv, logits_out_dev, n_nodes, workspace, ws_bytes, hip_stream, &ts);
@@ -752,6 +814,7 @@ psd_status psd_kv_compact_tree(psd_kv *kv, const int32_t *base_lens_dev, const i
                                int32_t path_stride, int32_t n_nodes, int32_t new_len_upper_bound, void *hip_stream) {
     if (!kv || !base_lens_dev || !path_dev || !path_len_dev) return PSD_ERR_NULL;
     if (n_nodes < 1 || n_nodes > kTreeMaxNodes || path_stride < n_nodes - 1) return PSD_ERR_SHAPE;
+    if (kv->q8) return PSD_ERR_UNIMPLEMENTED;
     if (base_lens_dev == kv->lens) return PSD_ERR_SHAPE;                       // the lengths are rewritten while blocks read the base
     const psd_model_desc &d = kv->m->d;
     const int cap = new_len_upper_bound < 0 || new_len_upper_bound > kv->len_ub ? kv->len_ub : new_len_upper_bound;
@@ -761,6 +824,175 @@ psd_status psd_kv_compact_tree(psd_kv *kv, const int32_t *base_lens_dev, const i
     const psd_status s = check_launch();
     if (s == PSD_OK) kv->len_ub = cap;
     return s;
+}
+
+// ---- rotary positions and the 8-bit cache by themselves
+
+psd_status psd_rope_create(const psd_rope_desc *desc, psd_rope **out) {
+    if (!desc || !out) return PSD_ERR_NULL;
+    const psd_rope_desc &d = *desc;
+    const int rot = d.rot_dim ? d.rot_dim : d.d_head;
+    if (d.d_head < 2 || d.d_head > kRopeMaxHead || d.d_head % 2 || rot < 2 || rot > d.d_head || rot % 2) return PSD_ERR_SHAPE;
+    if (d.layout != PSD_ROPE_HALF && d.layout != PSD_ROPE_INTERLEAVED) return PSD_ERR_SHAPE;
+    if (d.scaling < PSD_ROPE_PLAIN || d.scaling > PSD_ROPE_PARTS) return PSD_ERR_SHAPE;
+    auto positive = [](float x) { return x > 0.f && std::isfinite(x); };
+    if (!positive(d.theta) || !(d.magnitude >= 0.f) || !std::isfinite(d.magnitude)) return PSD_ERR_SHAPE;
+    if (d.scaling != PSD_ROPE_PLAIN && !positive(d.factor)) return PSD_ERR_SHAPE;
+    if (d.scaling == PSD_ROPE_PARTS && (!(d.low >= 0.f) || !(d.high > d.low) || !std::isfinite(d.high) || d.original_len <= 0)) return PSD_ERR_SHAPE;
+    psd_rope *r = new (std::nothrow) psd_rope;
+    if (!r) return PSD_ERR_NULL;
+    *r = psd_rope{};
+    r->d_head = d.d_head;
+    r->p = RopeParams{rot, d.layout == PSD_ROPE_INTERLEAVED, d.magnitude == 0.f ? 1.0f : d.magnitude};
+    const double two_pi = 6.283185307179586476925;
+    double theta = d.theta;
+    if (d.scaling == PSD_ROPE_BASE && rot > 2) theta *= std::pow((double)d.factor, (double)rot / (rot - 2));
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = std::pow(theta, -2.0 * i / rot);
+        if (d.scaling == PSD_ROPE_LINEAR) f /= d.factor;
+        if (d.scaling == PSD_ROPE_PARTS) {
+            const double w = (d.original_len * f / two_pi - d.low) / ((double)d.high - d.low);
+            const double kept = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+            f = kept * f + (1.0 - kept) * f / d.factor;
+        }
+        r->freq[i] = f;
+        r->turns.v[i] = f / two_pi;
+        if (!std::isfinite(f)) {
+            delete r;
+            return PSD_ERR_SHAPE;
+        }
+    }
+    *out = r;
+    return PSD_OK;
+}
+
+psd_status psd_rope_destroy(psd_rope *rope) {
+    if (!rope) return PSD_ERR_NULL;
+    delete rope;
+    return PSD_OK;
+}
+
+psd_status psd_rope_frequencies(const psd_rope *rope, double *out_host) {
+    if (!rope || !out_host) return PSD_ERR_NULL;
+    for (int i = 0; i < rope->p.rot / 2; ++i) out_host[i] = rope->freq[i];
+    return PSD_OK;
+}
+
+psd_status psd_model_set_rope(psd_model *m, const psd_rope *rope) {
+    if (!m) return PSD_ERR_NULL;
+    if (rope && rope->d_head != m->d.d_head) return PSD_ERR_SHAPE;
+    m->has_rope = rope != nullptr;
+    if (rope) m->rope = *rope;
+    return PSD_OK;
+}
+
+psd_status psd_rope_rotate(const psd_rope *rope, const void *x, void *y, const int32_t *positions, int32_t rows, int32_t n_heads,
+                           int32_t dtype, int64_t x_row_stride, int64_t y_row_stride, void *hip_stream) {
+    if (!rope) return PSD_ERR_NULL;
+    if (dtype != PSD_F32 && dtype != PSD_BF16) return PSD_ERR_DTYPE;
+    if (rows < 0 || n_heads <= 0 || n_heads > 65535) return PSD_ERR_SHAPE;
+    if (rows == 0) return PSD_OK;
+    if (!x || !y || !positions) return PSD_ERR_NULL;
+    const int64_t width = (int64_t)n_heads * rope->d_head;
+    if (x_row_stride < width || y_row_stride < width || (x == y && x_row_stride != y_row_stride)) return PSD_ERR_SHAPE;
+    if ((uintptr_t)x % elem_size(dtype) || (uintptr_t)y % elem_size(dtype) || (uintptr_t)positions % 4) return PSD_ERR_SHAPE;
+    RopeRotateArgs a{};
+    a.x = x; a.y = y; a.positions = positions; a.rows = rows; a.x_stride = x_row_stride; a.y_stride = y_row_stride;
+    a.heads = n_heads; a.d_h = rope->d_head; a.rope = rope->p; a.turns = rope->turns;
+    (void)hipGetLastError();
+    launch_rope_rotate(dtype, a, (hipStream_t)hip_stream);
+    return check_launch();
+}
+
+psd_status psd_kv8_layer(const psd_kv *kv, int32_t layer, psd_kv8_view *out) {
+    if (!kv || !out) return PSD_ERR_NULL;
+    if (!kv->q8) return PSD_ERR_DTYPE;
+    const psd_model_desc &d = kv->m->d;
+    if (layer < 0 || layer >= d.n_layers) return PSD_ERR_SHAPE;
+    const size_t heads = (size_t)layer * kv->batch * d.n_kv_heads, codes = heads * kv->max_len * d.d_head, scales = heads * (kv->max_len / kKv8Block);
+    *out = psd_kv8_view{(char *)kv->k + codes, (char *)kv->v + codes, kv->k_scale + scales, kv->v_scale + scales, kv->lens,
+                        kv->batch, d.n_kv_heads, d.d_head, kv->max_len};
+    return PSD_OK;
+}
+
+// what both calls on a layer check alike
+static psd_status check_kv8(const psd_kv8_view *c, int n_new, int n_q_heads, int len_upper_bound) {
+    if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->lens) return PSD_ERR_NULL;
+    if (c->d_head != 64 && c->d_head != 128) return PSD_ERR_SHAPE;
+    if (c->batch <= 0 || c->n_kv_heads <= 0 || (long)c->batch * c->n_kv_heads > 65535) return PSD_ERR_SHAPE;
+    if (c->max_len <= 0 || c->max_len % kKv8Block) return PSD_ERR_SHAPE;
+    if (n_new <= 0 || n_q_heads <= 0 || n_q_heads > 1024 || n_q_heads % c->n_kv_heads) return PSD_ERR_SHAPE;
+    if ((long)c->batch * n_new > (1L << 20) || (long)(n_q_heads / c->n_kv_heads) * n_new > (1L << 20)) return PSD_ERR_SHAPE;
+    if ((uintptr_t)c->k_codes % 16 || (uintptr_t)c->v_codes % 16 || (uintptr_t)c->k_scale % 4 || (uintptr_t)c->v_scale % 4) return PSD_ERR_SHAPE;
+    if (len_upper_bound < n_new || len_upper_bound > c->max_len) return PSD_ERR_CAPACITY;
+    return PSD_OK;
+}
+
+psd_status psd_kv8_append(const psd_kv8_view *cache, const psd_rope *rope, const void *q, const void *k, const void *v, void *q_out,
+                          int32_t n_new, int32_t n_q_heads, int32_t dtype, int64_t q_row_stride, int64_t k_row_stride,
+                          int64_t v_row_stride, int64_t q_out_row_stride, int32_t len_upper_bound, void *hip_stream) {
+    if (!k || !v || (q == nullptr) != (q_out == nullptr)) return PSD_ERR_NULL;
+    if (dtype != PSD_F32 && dtype != PSD_BF16) return PSD_ERR_DTYPE;
+    const psd_status s = check_kv8(cache, n_new, n_q_heads, len_upper_bound);
+    if (s != PSD_OK) return s;
+    if (rope && rope->d_head != cache->d_head) return PSD_ERR_SHAPE;
+    const int64_t kv_width = (int64_t)cache->n_kv_heads * cache->d_head, q_width = (int64_t)n_q_heads * cache->d_head;
+    if (k_row_stride < kv_width || v_row_stride < kv_width) return PSD_ERR_SHAPE;
+    if (q && (q_row_stride < q_width || q_out_row_stride < q_width || (q == q_out && q_row_stride != q_out_row_stride))) return PSD_ERR_SHAPE;
+    const size_t es = elem_size(dtype);
+    if ((uintptr_t)q % es || (uintptr_t)k % es || (uintptr_t)v % es || (uintptr_t)q_out % es) return PSD_ERR_SHAPE;
+    Kv8AppendArgs a{};
+    a.k_codes = (uint8_t *)cache->k_codes; a.v_codes = (uint8_t *)cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+    a.lens = cache->lens; a.q_out = q_out; a.q_out_stride = q_out_row_stride;
+    a.B = cache->batch; a.R = n_new; a.h_q = n_q_heads; a.h_kv = cache->n_kv_heads; a.d_h = cache->d_head; a.max_len = cache->max_len;
+    a.rope = rope ? rope->p : RopeParams{0, 0, 1.0f};
+    if (rope) a.turns = rope->turns;
+    (void)hipGetLastError();
+    launch_kv8_append(a, Kv8Source{q, k, v, q_row_stride, k_row_stride, v_row_stride, dtype == PSD_BF16, 0, 0}, (hipStream_t)hip_stream);
+    return check_launch();
+}
+
+// the splits' results, then their references and sums
+static size_t kv8_attention_scratch(int B, int R, int h_q, int d_h, int splits, size_t *ml) {
+    if (splits <= 1) return 0;
+    const size_t rows = (size_t)B * R * h_q * splits;
+    *ml = align256(rows * d_h * sizeof(float));
+    return *ml + align256(rows * sizeof(float2));
+}
+
+size_t psd_kv8_attention_workspace_bytes(int32_t batch, int32_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t d_head,
+                                         int32_t len_upper_bound) {
+    if (batch <= 0 || n_new <= 0 || n_kv_heads <= 0 || n_q_heads <= 0 || n_q_heads % n_kv_heads || len_upper_bound <= 0) return 0;
+    size_t ml = 0;
+    return kv8_attention_scratch(batch, n_new, n_q_heads, d_head, kv8_attn_splits(batch, n_new, n_q_heads, n_kv_heads, d_head, len_upper_bound, nullptr), &ml);
+}
+
+psd_status psd_kv8_attention(const psd_kv8_view *cache, const void *q, void *out, int32_t n_new, int32_t n_q_heads, float scale,
+                             int64_t q_row_stride, int64_t out_row_stride, int32_t len_upper_bound, void *workspace, size_t ws_bytes,
+                             void *hip_stream) {
+    if (!q || !out) return PSD_ERR_NULL;
+    const psd_status s = check_kv8(cache, n_new, n_q_heads, len_upper_bound);
+    if (s != PSD_OK) return s;
+    const int64_t width = (int64_t)n_q_heads * cache->d_head;
+    if (q_row_stride < width || out_row_stride < width || q_row_stride % 8 || out_row_stride % 8) return PSD_ERR_SHAPE;
+    if ((uintptr_t)q % 16 || (uintptr_t)out % 16 || !std::isfinite(scale)) return PSD_ERR_SHAPE;
+    Kv8AttnArgs a{};
+    a.q = q; a.q_stride = q_row_stride; a.q_bf16 = true;
+    a.k = (const uint8_t *)cache->k_codes; a.v = (const uint8_t *)cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+    a.lens = cache->lens; a.B = cache->batch; a.R = n_new; a.h_q = n_q_heads; a.h_kv = cache->n_kv_heads; a.d_h = cache->d_head;
+    a.max_len = cache->max_len; a.scale = scale == 0.f ? 1.0f / sqrtf((float)cache->d_head) : scale;
+    a.splits = kv8_attn_splits(a.B, a.R, a.h_q, a.h_kv, a.d_h, len_upper_bound, &a.range);
+    a.out_bf16 = (uint16_t *)out; a.out_stride = out_row_stride;
+    size_t ml = 0;
+    const size_t need = kv8_attention_scratch(a.B, a.R, a.h_q, a.d_h, a.splits, &ml);
+    if (need) {
+        if (!workspace || (uintptr_t)workspace % 256 || ws_bytes < need) return PSD_ERR_WORKSPACE;
+        a.part_o = (float *)workspace;
+        a.part_ml = (float2 *)((char *)workspace + ml);
+    }
+    (void)hipGetLastError();
+    launch_kv8_attention(a, (hipStream_t)hip_stream);
+    return check_launch();
 }
 
 psd_status psd_profile_enable(int32_t max_launches) {

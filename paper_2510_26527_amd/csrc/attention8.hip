@@ -1,0 +1,302 @@
+// Attention over the 8-bit KV cache (kv8.hip) on gfx950: out = softmax(scale * q K^T) V, row r of a sequence seeing positions
+// 0 .. len + r, in one pass over the keys with a running reference and sum.
+//
+// The codes become fp16, exactly, two an instruction, in the registers they were loaded into; both products run on the fp16
+// matrix cores.  A block's 64 keys share their scales, so K's multiplies the scores (with the softmax scale and log2 e, one number a
+// query and block) and V's is the unit that the output accumulates in, which moves where a block's differs from the one before.
+// Roundings: a query row is divided by the power of two that brings its largest entry to 1 .. 2 and rounded to fp16 (bf16 entries
+// down to 2^-17 of the row's largest stay exact, smaller ones are off by 2^-25 of it at most); the softmax weights are rounded to fp16, held at 2^10
+// times their size against the reference so that what a long cache adds up stays above fp16's smallest; sums, references and outputs are fp32.
+//
+// Operands without a transpose or LDS: a wavefront takes the scores of 64 keys as S^T = K q^T in four 16 x 16 tiles.  Row i of tile t
+// is key 16 (i / 4) + 4 t + i % 4, so that lane group g ends up with the scores of keys 16 g .. 16 g + 15 of its query: exactly the
+// order in which the other operand of P V, sixteen tokens of one entry, is one 16-byte load.
+#include <math.h>
+
+#include "common.h"
+#include "kernels.h"
+#include "prof.h"
+#include "../../include/psd.h"
+
+namespace psd {
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+constexpr float kFarBelow = -1.5e38f;      // the reference before a key was seen: finite, so that differences are numbers
+constexpr float kSlack = 5.f;              // the reference moves when a score is this far (in powers of two) above it
+constexpr float kLift = 10.f;              // weights are held times 2^kLift: at most 2^15, fp16 ends at 2^16
+
+// eight codes as one matrix operand, exact
+__device__ __forceinline__ f16x8 widen8(uint32_t lo, uint32_t hi) {
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// bytes of w that hold e4m3's NaN, as 0x80
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// ... and 0x80 bytes as fp16 ones
+__device__ __forceinline__ f16x8 nan_flags(uint32_t lo, uint32_t hi) {
+    return widen8((lo >> 7) * 0x38u, (hi >> 7) * 0x38u);     // 0x38 is 1.0
+}
+__device__ __forceinline__ f32x8 load_q8(const Kv8AttnArgs &a, int64_t at) {
+    if (a.q_bf16) {
+        const uint16_t *p = (const uint16_t *)a.q + at;
+        f32x8 v;
+        const u32x4 raw = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? __uint_as_float(raw[j >> 1] & 0xffff0000u) : __uint_as_float(raw[j >> 1] << 16);
+        return v;
+    }
+    return load_f32x8((const float *)a.q + at);
+}
+// a finished result's entries d .. d + 3 of query head `head` of row m
+__device__ __forceinline__ void store_out4(const Kv8AttnArgs &a, int64_t m, int head, int d, f32x4 r) {
+    const int col = head * a.d_h + d;
+    if (a.out_bf16) *reinterpret_cast<uint2 *>(a.out_bf16 + m * a.out_stride + col) = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
+    const int64_t at = m * a.h_q * a.d_h + col;
+    if (a.out) *reinterpret_cast<f32x4 *>(a.out + at) = r;
+    if (a.out16)
+        *reinterpret_cast<uint2 *>(a.out16 + at) = make_uint2(f32_to_f16_bits(r[0]) | ((uint32_t)f32_to_f16_bits(r[1]) << 16),
+                                                             f32_to_f16_bits(r[2]) | ((uint32_t)f32_to_f16_bits(r[3]) << 16));
+    if (a.out_op) op_store4(a.out_op, (int)m, col, a.op_folded, r);
+}
+
+// One wavefront's part of a query tile of 16 rows: scores, weights and products over whole blocks of 64 keys.
+template <int DH>
+struct QueryTile {
+    static constexpr int KS = DH / 32, DT = DH / 16;
+    f16x8 q[KS];                  // lane (query i, group g): entries 64 (s / 2) + 16 g + 8 (s % 2) .. + 7
+    float unit;                   // what a score has to be multiplied with, but for K's scale, to be in powers of two
+    int limit;                    // the last position that the row sees; -1: no row
+    float m, l;                   // reference; sum of this lane's weights, times 2^kLift
+    f32x4 o[DT];                  // lane (query i, group g): entries 16 dt + 4 g .. + 3, in units of V's scale `vref`
+
+    __device__ __forceinline__ void init(const Kv8AttnArgs &a, int64_t row, int head, int limit_, int g, float scale_log2) {
+        limit = limit_;
+        m = kFarBelow;
+        l = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        f32x8 v[KS];
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            v[s] = load_q8(a, row * a.q_stride + head * DH + 64 * (s >> 1) + 16 * g + 8 * (s & 1));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[s][j]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const int e = min(max((int)(__float_as_uint(top) >> 23), 1), 253);                 // 2^(e - 127) <= top
+        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+        unit = scale_log2 * __uint_as_float((uint32_t)e << 23);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = __builtin_bit_cast(f16x8, f32x8_to_f16x8(v[s] * down));
+    }
+};
+
+// Few query rows: the wavefronts of a block share its 16 query rows and take every fourth block of 64 keys each; their results are
+// joined in LDS, and those of a sequence's splits by the combine kernel.
+template <int DH>
+__global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float scale_log2) {
+    constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64;
+    __shared__ float s_o[4][16][DH + 4];
+    __shared__ float s_m[4][16], s_l[4][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+    const int split = blockIdx.x, b = blockIdx.z / a.h_kv, hk = blockIdx.z % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
+    const int len = min(max(a.lens[b], 0), a.max_len);
+    const int n_keys = min(len + a.R, a.max_len);
+    const int qi = blockIdx.y * 16 + i;
+    const int row = (qi < NQ ? qi : NQ - 1) % a.R, head = hk * group + (qi < NQ ? qi : NQ - 1) / a.R;
+    QueryTile<DH> t;
+    t.init(a, (int64_t)b * a.R + row, head, qi < NQ ? len + row : -1, g, scale_log2);
+    const int seen = min(len + chunk_last_row(blockIdx.y, 16, a.R, group) + 1, n_keys);    // no row of the block sees past it
+    const int all_see = len + (((int)blockIdx.y * 16) / a.R == (min((int)blockIdx.y * 16 + 16, NQ) - 1) / a.R ? ((int)blockIdx.y * 16) % a.R : 0) + 1;
+    const int n_blocks = (seen + kKv8Block - 1) / kKv8Block;
+    const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
+    const size_t cache_row = (size_t)b * a.h_kv + hk;
+    const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
+    const float *ks = a.k_scale + cache_row * (a.max_len / kKv8Block), *vs = a.v_scale + cache_row * (a.max_len / kKv8Block);
+    float vref = 1.f;
+
+    for (int kb = first + wave; kb < last; kb += 4) {
+        u32x4 kr[4][KL], vr[DT];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int j = 0; j < KL; ++j)
+                kr[c][j] = *reinterpret_cast<const u32x4 *>(K + ((size_t)kb * 64 + 16 * (i >> 2) + 4 * c + (i & 3)) * DH + 64 * j + 16 * g);
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+            vr[dt] = *reinterpret_cast<const u32x4 *>(V + (size_t)kb * 64 * DH + (dt * 16 + i) * 64 + 16 * g);
+        const float k_scale = ks[kb], v_scale = vs[kb];
+        f32x4 s[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < KS; ++e)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                s[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(kr[c][e >> 1][2 * (e & 1)], kr[c][e >> 1][2 * (e & 1) + 1]), t.q[e], s[c], 0, 0, 0);
+        const float f = t.unit * k_scale;
+        float top = -INFINITY;
+        const bool masked = kb * 64 + 64 > all_see;          // (the same for the whole block)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[c][e] *= f;
+                if (masked && kb * 64 + 16 * g + 4 * c + e > t.limit) s[c][e] = -INFINITY;
+                top = fmaxf(top, s[c][e]);
+            }
+        if (__ballot(top > t.m + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float m = top > t.m + kSlack ? top : t.m, shrink = __builtin_amdgcn_exp2f(t.m - m);
+            t.m = m;
+            t.l *= shrink;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) t.o[dt] *= shrink;
+        }
+        if (v_scale != vref) {
+            const float to = vref / v_scale;
+            vref = v_scale;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) t.o[dt] *= to;
+        }
+        f16x8 p[2];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float w = __builtin_amdgcn_exp2f(s[c][e] - (t.m - kLift));
+                t.l += w;
+                p[c >> 1][4 * (c & 1) + e] = (_Float16)w;
+            }
+        if (masked) {
+            // A position that some row does not see may hold anything.  What is no number there must not reach the product, where a
+            // weight of 0 would not keep it out; rows that see it get theirs from the flags.
+            uint32_t any = 0;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) any |= nan_codes(vr[dt][e]);
+            if (__ballot(any != 0)) {
+                f16x8 see[2];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) see[c >> 1][4 * (c & 1) + e] = (_Float16)(kb * 64 + 16 * g + 4 * c + e > t.limit ? 0.f : 1.f);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                    f32x4 hit{0.f, 0.f, 0.f, 0.f};
+                    uint32_t n[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { n[e] = nan_codes(vr[dt][e]); vr[dt][e] &= ~((n[e] >> 7) * 0xffu); }
+                    hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(nan_flags(n[0], n[1]), see[0], hit, 0, 0, 0);
+                    hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(nan_flags(n[2], n[3]), see[1], hit, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (hit[e] > 0.f) t.o[dt][e] = __uint_as_float(0x7fc00000u);
+                }
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+            t.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(vr[dt][0], vr[dt][1]), p[0], t.o[dt], 0, 0, 0);
+            t.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(vr[dt][2], vr[dt][3]), p[1], t.o[dt], 0, 0, 0);
+        }
+    }
+
+    // join the wavefronts, in their order
+    float l = t.l;
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    if (g == 0) { s_m[wave][i] = t.m; s_l[wave][i] = l; }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4 *>(&s_o[wave][i][dt * 16 + 4 * g]) = t.o[dt] * vref;
+    __syncthreads();
+    for (int x = tid; x < 16 * (DH / 4); x += 256) {
+        const int qc = x / (DH / 4), d = x % (DH / 4) * 4, q = blockIdx.y * 16 + qc;
+        if (q >= NQ) continue;
+        const float M = fmaxf(fmaxf(s_m[0][qc], s_m[1][qc]), fmaxf(s_m[2][qc], s_m[3][qc]));
+        float L = 0.f;
+        f32x4 r{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s_m[w][qc] - M);
+            L += s_l[w][qc] * f;
+            r += *reinterpret_cast<const f32x4 *>(&s_o[w][qc][d]) * f;
+        }
+        if (L != 0.f) r = r * (1.0f / L);                    // (a split none of whose keys the row sees: 0)
+        const int64_t m = (int64_t)b * a.R + q % a.R;
+        const int h = hk * group + q / a.R;
+        if (a.splits == 1) {
+            store_out4(a, m, h, d, r);
+        } else {
+            const size_t at = ((size_t)m * a.h_q + h) * a.splits + split;
+            *reinterpret_cast<f32x4 *>(a.part_o + at * DH + d) = r;
+            if (d == 0) a.part_ml[at] = make_float2(M, L);
+        }
+    }
+}
+
+// Joins the splits of a row and head, in their order: 64 / (d_h / 4) of them a wavefront, four entries a lane.
+template <int DH>
+__global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
+    constexpr int kLanes = DH / 4, kRows = 256 / kLanes;
+    const int64_t rh = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
+    if (rh >= (int64_t)a.B * a.R * a.h_q) return;
+    const int d = threadIdx.x % kLanes * 4;
+    const float2 *ml = a.part_ml + rh * a.splits;
+    const float *o = a.part_o + rh * a.splits * DH + d;
+    float M = ml[0].x;
+    for (int s = 1; s < a.splits; ++s) M = fmaxf(M, ml[s].x);
+    float L = 0.f;
+    f32x4 r{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 e = ml[s];
+        const float w = e.y * __builtin_amdgcn_exp2f(e.x - M);
+        L += w;
+        r += *reinterpret_cast<const f32x4 *>(o + (size_t)s * DH) * w;
+    }
+    store_out4(a, rh / a.h_q, (int)(rh % a.h_q), d, r * (1.0f / L));
+}
+
+}  // namespace
+
+int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
+    const int NQ = h_q / h_kv * R, chunks = (NQ + 15) / 16, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
+    long splits = 512 / ((long)B * h_kv * chunks);
+    const int most = (blocks + 3) / 4;
+    splits = splits > most ? most : splits;
+    return splits < 1 ? 1 : (int)splits;
+}
+
+int kv8_attn_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound, int *range) {
+    const int blocks = (len_bound + kKv8Block - 1) / kKv8Block, splits = kv8_attn_max_splits(B, R, h_q, h_kv, d_h, len_bound);
+    const int r = (int)((blocks + splits - 1) / splits);
+    if (range) *range = r;
+    return (blocks + r - 1) / r;
+}
+
+void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
+    const float scale_log2 = 1.4426950408889634f * a.scale;
+    const int NQ = a.h_q / a.h_kv * a.R;
+    {
+        ScopedProf sp(PSD_KIND_ATTN, stream);
+        const dim3 grid(a.splits, (NQ + 15) / 16, a.B * a.h_kv);
+        if (a.d_h == 128) launch_kernel(attn8_direct_kernel<128>, grid, 256, 0, stream, a, scale_log2);
+        else launch_kernel(attn8_direct_kernel<64>, grid, 256, 0, stream, a, scale_log2);
+    }
+    if (a.splits > 1) {
+        ScopedProf sp(PSD_KIND_ATTN_COMBINE, stream);
+        const int64_t rows = (int64_t)a.B * a.R * a.h_q, per = 256 / (a.d_h / 4);
+        const unsigned grid = (unsigned)((rows + per - 1) / per);
+        if (a.d_h == 128) launch_kernel(attn8_combine_kernel<128>, grid, 256, 0, stream, a);
+        else launch_kernel(attn8_combine_kernel<64>, grid, 256, 0, stream, a);
+    }
+}
+
+}  // namespace psd

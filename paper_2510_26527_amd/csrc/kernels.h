@@ -222,6 +222,89 @@ void launch_kv_compact_tree(int dtype, void *k, void *v, int32_t *lens, const in
 void launch_probe_read(const void *src, size_t bytes, void *sink, int blocks, hipStream_t stream);
 void launch_probe_mfma(const void *seed, void *sink, int blocks, int iters, hipStream_t stream);
 
+// ---------------------------------------------------------------- rotary positions (rope.hip)
+constexpr int kRopeMaxHead = 256;          // entries of a head
+struct RopeParams {
+    int rot;                      // entries that turn
+    int interleaved;              // pairs (2i, 2i + 1); else (i, i + rot / 2)
+    float magnitude;              // of cos and sin
+};
+struct RopeTurns { double v[kRopeMaxHead / 2]; };      // frequencies / (2 pi)
+// n / d of unsigned numbers below 2^31 by a multiplication: with 2^(s-1) < d <= 2^s, mul = ceil(2^(31+s) / d) < 2^32 is off by less
+// than one in 2^s, which adds less than 1 / d to the quotient of an n below 2^31
+struct FastDiv {
+    uint32_t n, mul, shift;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t d) : n(d), mul(0), shift(0) {
+        while ((1ull << shift) < d) ++shift;
+        mul = (uint32_t)(((1ull << (31 + shift)) + d - 1) / d);
+    }
+    __host__ __device__ __forceinline__ uint32_t div(uint32_t x) const { return (uint32_t)((uint64_t)x * mul >> (31 + shift)); }
+};
+struct RopeRotateArgs {
+    const void *x;                // [rows][heads][d_h], rows x_stride elements apart
+    void *y;
+    const int32_t *positions;     // [rows]
+    int64_t rows, x_stride, y_stride;
+    int heads, d_h;
+    RopeParams rope;
+    int block_rows;               // these three: set by launch_rope_rotate
+    FastDiv per_row, per_head;
+    RopeTurns turns;
+};
+void launch_rope_rotate(int dtype, RopeRotateArgs a, hipStream_t stream);
+// cs[m][i], i < rot / 2, rows `stride` pairs apart: of position lens[m / R] + m % R (tree: + the node's depth)
+void launch_rope_table(float2 *cs, int stride, const int32_t *lens, int M, int R, const RopeParams &rope, const RopeTurns &turns,
+                       const TreeShape *tree, hipStream_t stream);
+
+// ---------------------------------------------------------------- 8-bit KV cache (kv8.hip, attention8.hip)
+constexpr int kKv8Block = 64;              // tokens that share a scale
+struct Kv8AppendArgs {
+    uint8_t *k_codes, *v_codes;   // one layer: [B][h_kv][max_len][d_h], [B][h_kv][max_len / 64][d_h][64]
+    float *k_scale, *v_scale;     // [B][h_kv][max_len / 64]
+    const int32_t *lens;          // [B] valid positions before this step
+    void *q_out;                  // rotated queries, rows q_out_stride elements apart; NULL: no queries
+    int64_t q_out_stride;
+    int B, R, h_q, h_kv, d_h, max_len;
+    int units;                    // these two: set by launch_kv8_append
+    bool q_vec;
+    RopeParams rope;              // rot 0: nothing turns
+    const float2 *cs;             // the rows' (cos, sin), rows cs_stride pairs apart; NULL: worked out from `turns`
+    int cs_stride;
+    RowScale rs;
+    RopeTurns turns;
+};
+// where the step's rows lie: row b * R + r, heads side by side
+struct Kv8Source {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;      // elements between rows
+    bool bf16;
+    int slots;                    // > 0: fp32 partial sums, this many slots slot_stride elements apart, rows 16-byte aligned
+    int64_t slot_stride;
+};
+void launch_kv8_append(const Kv8AppendArgs &a, const Kv8Source &src, hipStream_t stream);
+struct Kv8AttnArgs {
+    const void *q;                // [B][R][h_q][d_h] rotated queries, rows q_stride elements apart
+    int64_t q_stride;
+    bool q_bf16;                  // else fp32
+    const uint8_t *k, *v;         // codes and scales of one layer
+    const float *k_scale, *v_scale;
+    const int32_t *lens;          // [B] valid positions BEFORE this step, whose rows are in the cache already
+    int B, R, h_q, h_kv, d_h, max_len;
+    float scale;                  // of the scores
+    int splits, range;            // kv8_attn_plan: keys of a split, in blocks of 64
+    uint16_t *out_bf16;           // one of the four, rows out_stride elements apart where it says so
+    int64_t out_stride;
+    float *out;                   // [B][R][h_q * d_h]
+    uint16_t *out16, *out_op;     // as AttnArgs
+    bool op_folded;
+    float *part_o;                // [B][R][h_q][splits][d_h], a split's normalised result
+    float2 *part_ml;              // [B][R][h_q][splits] (reference, sum of weights)
+};
+int kv8_attn_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound, int *range);
+int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound);      // of any cache up to len_bound
+void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream);
+
 // ---------------------------------------------------------------- row-wise kernels (rowwise.hip)
 // optional by-product of the embedding kernel: cs[m][i] = (cos, sin) of (the position of row m) * theta^(-2i/d_h)
 struct RopeTable {
@@ -247,10 +330,11 @@ void launch_embed_norm(int dtype, const void *embed, const int32_t *tokens, floa
                        float *sumsq_out, int M, int d, int vocab, float eps, RopeTable rt, uint16_t *xn16, OpRows op, ZeroFill zf,
                        const TreeShape *tree, uint32_t *tree_anc, hipStream_t stream);
 // qkv = sum over splits of partial [S][M][(h_q+2h_kv) d_h] -> rotated q (fp32), rotated k and v appended
-// to the cache (model dtype); cs_table: RopeTable::cs of these rows, NULL: the angles are evaluated again
+// to the cache (model dtype); cs_table: RopeTable::cs of these rows, NULL: the angles are evaluated again; pairs: how entries pair (needs
+// cs_table), NULL: (i, i + d_h / 2)
 void launch_reduce_rope_append(int dtype, const float *partial, int S, RowScale rs, float *q_out, void *k_cache,
                                void *v_cache, const int32_t *lens, int B, int R, int h_q, int h_kv, int d_h,
-                               int max_len, float theta, const float2 *cs_table, hipStream_t stream);
+                               int max_len, float theta, const float2 *cs_table, const RopeParams *pairs, hipStream_t stream);
 // x += sum over splits of partial [S][M][d]; xn = rmsnorm(x) * gain (xn16, if given: the same rounded to fp16; xn may be NULL
 // beside that or op)
 void launch_reduce_residual_norm(int dtype, const float *partial, int S, float *x, const void *gain, float *xn,

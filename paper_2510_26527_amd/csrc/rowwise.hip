@@ -148,12 +148,13 @@ __global__ __launch_bounds__(kRowThreads) void residual_norm_kernel(const TW *em
 // One block per (new row, head slot): slots 0..h_q-1 rotate a query head, the next h_kv rotate a
 // key head into the cache, the last h_kv copy a value head into the transposed V cache.  The
 // projection arrives as split-K partials and is summed here, in split order.  Thread i < d_h/2
-// owns the rotation pair (i, i + d_h/2); the angle position * theta^(-2i/d_h) is evaluated in fp64.
-template <typename TC>
+// owns the rotation pair (i, i + d_h/2); the angle position * theta^(-2i/d_h) is evaluated in fp64.  PAIRS (a model whose rotary
+// positions pair entries differently, or turn part of a head): thread i has the i-th pair, or, behind the rotated part, two entries that stay.
+template <typename TC, bool PAIRS = false>
 __global__ __launch_bounds__(64) void reduce_rope_append_kernel(const float *partial, int S, size_t split_stride,
                                                                 RowScale rs, float *q_out, TC *k_cache, TC *v_cache,
                                                                 const int32_t *lens, int R, int h_q, int h_kv, int d_h,
-                                                                int max_len, float theta, const float2 *cs_table) {
+                                                                int max_len, float theta, const float2 *cs_table, RopeParams rope) {
     const int m = blockIdx.x, slot = blockIdx.y, b = m / R, r = m % R;
     const int pos = lens[b] + r;
     if (pos >= max_len) return;            // capacity was checked on the host; never write outside
@@ -178,11 +179,19 @@ __global__ __launch_bounds__(64) void reduce_rope_append_kernel(const float *par
     };
     auto scale_of = [&]() { return rs.sumsq ? 1.0f / sqrtf(wave_sum(ssq) * rs.inv_d + rs.eps) : 1.0f; };
     if (slot < h_q + h_kv) {
-        const float r1 = i < half ? value(i) : 0.f, r2 = i < half ? value(half + i) : 0.f;
+        int e1 = i, e2 = half + i;
+        if constexpr (PAIRS) {
+            if (2 * i >= rope.rot || rope.interleaved) { e1 = 2 * i; e2 = 2 * i + 1; }
+            else e2 = i + rope.rot / 2;
+        }
+        const float r1 = i < half ? value(e1) : 0.f, r2 = i < half ? value(e2) : 0.f;
         const float sc = scale_of();
         if (i >= half) return;
         float c, s;
-        if (cs_table) {
+        if (PAIRS && 2 * i >= rope.rot) {
+            c = 1.f;
+            s = 0.f;
+        } else if (cs_table) {
             const float2 t = cs_table[(size_t)m * half + i];
             c = t.x;
             s = t.y;
@@ -197,12 +206,12 @@ __global__ __launch_bounds__(64) void reduce_rope_append_kernel(const float *par
         const float y1 = x1 * c - x2 * s, y2 = x2 * c + x1 * s;
         if (slot < h_q) {
             float *dst = q_out + ((size_t)m * h_q + slot) * d_h;
-            dst[i] = y1;
-            dst[half + i] = y2;
+            dst[e1] = y1;
+            dst[e2] = y2;
         } else {
             TC *dst = k_cache + (((size_t)b * h_kv + (slot - h_q)) * max_len + pos) * d_h;
-            store_elem(dst, i, y1);
-            store_elem(dst, half + i, y2);
+            store_elem(dst, e1, y1);
+            store_elem(dst, e2, y2);
         }
     } else {
         // V is stored transposed: v_cache[b][h][d][pos]
@@ -394,10 +403,18 @@ void launch_reduce_residual_norm(int dtype, const float *partial, int S, float *
 
 void launch_reduce_rope_append(int dtype, const float *partial, int S, RowScale rs, float *q_out, void *k_cache,
                                void *v_cache, const int32_t *lens, int B, int R, int h_q, int h_kv, int d_h,
-                               int max_len, float theta, const float2 *cs_table, hipStream_t stream) {
+                               int max_len, float theta, const float2 *cs_table, const RopeParams *pairs, hipStream_t stream) {
     ScopedProf sp(PSD_KIND_ROPE_APPEND, stream);
     const size_t stride = (size_t)B * R * (h_q + 2 * h_kv) * d_h;
     const dim3 grid(B * R, h_q + 2 * h_kv);
+    if (pairs) {
+        auto go = [&](auto kernel, auto *k, auto *v) {
+            launch_kernel(kernel, grid, 64, 0, stream, partial, S, stride, rs, q_out, k, v, lens, R, h_q, h_kv, d_h, max_len, theta, cs_table, *pairs);
+        };
+        if (dtype == PSD_BF16) go(reduce_rope_append_kernel<uint16_t, true>, (uint16_t *)k_cache, (uint16_t *)v_cache);
+        else go(reduce_rope_append_kernel<float, true>, (float *)k_cache, (float *)v_cache);
+        return;
+    }
     if (dtype == PSD_BF16 && !rs.sumsq && cs_table) {
         const int per = 1024 / (d_h / 2);                                   // query and key heads per block
         const int qk = B * R * ((h_q + h_kv + per - 1) / per);
@@ -408,10 +425,10 @@ void launch_reduce_rope_append(int dtype, const float *partial, int S, RowScale 
     }
     if (dtype == PSD_BF16)
         launch_kernel(reduce_rope_append_kernel<uint16_t>, grid, 64, 0, stream, partial, S, stride, rs, q_out, (uint16_t *)k_cache,
-                                                                     (uint16_t *)v_cache, lens, R, h_q, h_kv, d_h, max_len, theta, cs_table);
+                                                                     (uint16_t *)v_cache, lens, R, h_q, h_kv, d_h, max_len, theta, cs_table, RopeParams{});
     else
         launch_kernel(reduce_rope_append_kernel<float>, grid, 64, 0, stream, partial, S, stride, rs, q_out, (float *)k_cache, (float *)v_cache,
-                                                                  lens, R, h_q, h_kv, d_h, max_len, theta, cs_table);
+                                                                  lens, R, h_q, h_kv, d_h, max_len, theta, cs_table, RopeParams{});
 }
 
 void launch_reduce_swiglu(const float *partial, int S, RowScale rs, float *h, int M, int f, uint16_t *h16, hipStream_t stream) {

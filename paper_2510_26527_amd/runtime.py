@@ -45,6 +45,14 @@ class Model:
                                                   [self.quant[n][1].data_ptr() for n in names])
         self._ws = None
         self.packed = None
+        self.rope = None
+
+    def set_rope(self, rope):
+        """Turn by `rope` (a Rope, None: by the shape's rope_theta) in every forward from now on."""
+        psd.psd_model_set_rope(self.handle, None if rope is None else rope.handle)
+        self.rope = rope
+        self._ws = None
+        return self
 
     def pack(self):
         """Build the streaming copy of the projection weights (bf16 models) for steps of up to 128 rows."""
@@ -107,6 +115,187 @@ class KVCache:
         if self.handle is not None:
             psd.psd_kv_destroy(self.handle)
             self.handle = None
+
+
+def _current(t):
+    """The library enqueues on the current device: a tensor of another one is the caller's mistake."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensor on {t.device}, the current device is {torch.cuda.current_device()}")
+
+
+def _row_stride(t, rows):
+    """Elements between the rows of t [..., heads, d], whose heads are dense within a row, and rows evenly apart."""
+    if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1]):
+        raise ValueError("a row's heads have to lie side by side")
+    stride, span = None, 1
+    for n, st in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+        if n > 1:
+            if stride is None:
+                stride = st
+            elif st != stride * span:
+                raise ValueError("rows have to be evenly apart")
+            span *= n
+    if span != rows:
+        raise ValueError(f"{rows} rows expected, got {tuple(t.shape[:-2])}")
+    return t.shape[-2] * t.shape[-1] if stride is None else stride
+
+
+class Rope:
+    """A psd_rope: how query and key heads turn by their positions."""
+
+    _LAYOUT = {"half": psd.PSD_ROPE_HALF, "interleaved": psd.PSD_ROPE_INTERLEAVED}
+    _SCALING = {"none": psd.PSD_ROPE_PLAIN, "linear": psd.PSD_ROPE_LINEAR, "base": psd.PSD_ROPE_BASE, "parts": psd.PSD_ROPE_PARTS}
+
+    def __init__(self, d_head, rot_dim=None, layout="half", theta=1.0e4, scaling="none", factor=1.0, low=1.0, high=4.0,
+                 original_len=0, magnitude=1.0):
+        self.handle = None
+        self.d_head, self.rot_dim = d_head, d_head if rot_dim is None else rot_dim
+        self.handle = psd.psd_rope_create(psd.psd_rope_desc(d_head, self.rot_dim, self._LAYOUT[layout], self._SCALING[scaling], theta,
+                                                            factor, low, high, original_len, magnitude))
+
+    def frequencies(self):
+        return psd.psd_rope_frequencies(self.handle, self.rot_dim // 2)
+
+    def rotate(self, x, positions, out=None, stream=None):
+        """x [..., heads, d_head] (fp32 or bf16), positions int32 of its leading shape -> a new tensor, or `out` (which may be x)."""
+        _current(x)
+        rows = positions.numel()
+        if x.shape[:-2] != positions.shape or x.shape[-1] != self.d_head or positions.dtype != torch.int32 or not positions.is_contiguous():
+            raise ValueError("x [..., heads, d_head] with contiguous int32 positions [...] expected")
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        elif out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError("out has another shape or type than x")
+        if positions.device != x.device or out.device != x.device:
+            raise ValueError("tensors on different devices")
+        if rows:
+            psd.psd_rope_rotate(self.handle, x, out, positions, rows, x.shape[-2], psd.dtype_code(x.dtype), _row_stride(x, rows),
+                                _row_stride(out, rows), stream)
+        return out
+
+    def close(self):
+        if self.handle is not None:
+            psd.psd_rope_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+
+class KVCache8:
+    """An 8-bit cache: e4m3 codes k [L,B,h_kv,max_len,d_h] and v [L,B,h_kv,max_len/64,d_h,64], their scales [L,B,h_kv,max_len/64],
+    the device length vector, and the psd_kv handle over them.  Goes wherever a KVCache goes, but for token trees."""
+
+    def __init__(self, model: Model, batch, max_len, fill_garbage=False):
+        s = model.shape
+        self.model, self.batch, self.max_len = model, batch, max_len
+        lead = (s.n_layers, batch, s.n_kv_heads)
+        make = (lambda shape, dt: torch.full(shape, 255 if dt == torch.uint8 else float("nan"), dtype=dt, device=model.device)) \
+            if fill_garbage else (lambda shape, dt: torch.empty(shape, dtype=dt, device=model.device))
+        self.k = make(lead + (max_len, s.d_head), torch.uint8)
+        self.v = make(lead + (max_len // 64, s.d_head, 64), torch.uint8)
+        self.k_scale = make(lead + (max_len // 64,), torch.float32)
+        self.v_scale = make(lead + (max_len // 64,), torch.float32)
+        self.lens = torch.zeros(batch, dtype=torch.int32, device=model.device)
+        self._create(0)
+
+    def _create(self, bound):
+        self.handle = psd.psd_kv_create_q8(self.model.handle, self.batch, self.max_len, self.k, self.v, self.k_scale, self.v_scale,
+                                           self.lens, bound)
+
+    def load(self, k_layers, v_layers, lens):
+        """Quantise given contents in: per-layer [B, h_kv, n_ctx, d_h] tensors whose keys are rotated already, lens the valid length
+        per sequence (int or list)."""
+        n_ctx = k_layers[0].shape[2]
+        self.lens.zero_()
+        psd.psd_kv_destroy(self.handle)
+        self.handle = None
+        self._create(0)
+        for l, (k, v) in enumerate(zip(k_layers, v_layers)):
+            rows = [t.to(self.model.device).transpose(1, 2).contiguous() for t in (k, v)]
+            if n_ctx:
+                self.layer(l).append(None, rows[0], rows[1], None, len_upper_bound=n_ctx)
+        lens_t = torch.as_tensor(lens, dtype=torch.int32).expand(self.batch).contiguous()
+        self.lens.copy_(lens_t)
+        psd.psd_kv_destroy(self.handle)
+        self.handle = None
+        self._create(int(lens_t.max()))
+
+    def layer(self, l):
+        """One layer, for programs that append and attend by themselves."""
+        return KV8Layer(self.k[l], self.v[l], self.k_scale[l], self.v_scale[l], self.lens)
+
+    def close(self):
+        if self.handle is not None:
+            psd.psd_kv_destroy(self.handle)
+            self.handle = None
+
+
+class KV8Layer:
+    """One layer of an 8-bit cache over the caller's tensors: codes uint8 k [B, h_kv, max_len, d_h] and v [B, h_kv, max_len/64, d_h, 64],
+    scales fp32 [B, h_kv, max_len/64], lens int32 [B]."""
+
+    def __init__(self, k, v, k_scale, v_scale, lens):
+        B, h, n, d = k.shape
+        if tuple(v.shape) != (B, h, n // 64, d, 64) or tuple(k_scale.shape) != (B, h, n // 64) or k_scale.shape != v_scale.shape:
+            raise ValueError("codes and scales do not belong together")
+        if k.dtype != torch.uint8 or v.dtype != torch.uint8 or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+            raise ValueError("codes are uint8, scales float32")
+        if tuple(lens.shape) != (B,) or lens.dtype != torch.int32 or not all(t.is_contiguous() and t.device == k.device for t in (k, v, k_scale, v_scale, lens)):
+            raise ValueError("lens is int32 [B], and every tensor contiguous and on one device")
+        self.k, self.v, self.k_scale, self.v_scale, self.lens = k, v, k_scale, v_scale, lens
+        self.view = psd.psd_kv8_view(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), lens.data_ptr(), B, h, d, n)
+
+    def append(self, q, k, v, rope=None, len_upper_bound=None, q_out=None, stream=None):
+        """Rows q [B, n_new, h_q, d_h] (or None), k and v [B, n_new, h_kv, d_h], all fp32 or all bf16, at positions lens[b] ..: rotated
+        by `rope` and quantised into the cache -> the rotated queries.  len_upper_bound: a bound of lens[b] + n_new."""
+        _current(k)
+        B, n, h, d = k.shape
+        if (B, h, d) != (self.view.batch, self.view.n_kv_heads, self.view.d_head) or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v are [B, n_new, n_kv_heads, d_head] of one type")
+        rows, q_stride, out_stride, h_q = B * n, 0, 0, h
+        if q is not None:
+            if q.shape[:2] != k.shape[:2] or q.shape[3] != d or q.dtype != k.dtype:
+                raise ValueError("q is [B, n_new, n_q_heads, d_head] of k's type")
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+                raise ValueError("q_out has another shape or type than q")
+            h_q, q_stride, out_stride = q.shape[2], _row_stride(q, rows), _row_stride(q_out, rows)
+        for t in (q, v, q_out, self.k):
+            if t is not None and t.device != k.device:
+                raise ValueError("tensors on different devices")
+        psd.psd_kv8_append(self.view, None if rope is None else rope.handle, q, k, v, q_out, n, h_q, psd.dtype_code(k.dtype), q_stride,
+                           _row_stride(k, rows), _row_stride(v, rows), out_stride,
+                           self.view.max_len if len_upper_bound is None else len_upper_bound, stream)
+        return q_out
+
+
+class KV8Attention:
+    """Workspace of psd_kv8_attention, reused across calls (on one stream at a time)."""
+
+    def __init__(self):
+        self._ws = None
+
+    def __call__(self, cache: KV8Layer, q, scale=0.0, len_upper_bound=None, out=None, stream=None):
+        """q bf16 [B, n_new, h_q, d_h], the rows just appended to `cache` -> bf16 of the same shape; scale 0: 1 / sqrt(d_h).
+        len_upper_bound: a bound of lens[b] + n_new."""
+        _current(q)
+        B, n, h_q, d = q.shape
+        view = cache.view
+        if (B, d) != (view.batch, view.d_head) or q.dtype != torch.bfloat16:
+            raise ValueError("q is bf16 [B, n_new, n_q_heads, d_head]")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out has another shape or type than q")
+        if cache.k.device != q.device or out.device != q.device:
+            raise ValueError("tensors on different devices")
+        bound = view.max_len if len_upper_bound is None else len_upper_bound
+        need = psd.psd_kv8_attention_workspace_bytes(B, n, h_q, view.n_kv_heads, d, bound)
+        if need and (self._ws is None or self._ws.numel() < need or self._ws.device != q.device):
+            self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+        psd.psd_kv8_attention(view, q, out, n, h_q, scale, _row_stride(q, B * n), _row_stride(out, B * n), bound, self._ws, stream)
+        return out
 
 
 def forward(model: Model, kv: KVCache, tokens, n_logit_rows=None, logits_out=None, stream=None):
