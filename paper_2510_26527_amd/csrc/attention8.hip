@@ -22,10 +22,12 @@ namespace psd {
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
 
 constexpr float kFarBelow = -1.5e38f;      // the reference before a key was seen: finite, so that differences are numbers
 constexpr float kSlack = 5.f;              // the reference moves when a score is this far (in powers of two) above it
-constexpr float kLift = 10.f;              // weights are held times 2^kLift: at most 2^15, fp16 ends at 2^16
+constexpr float kSlackV = 8.f;             // ... and the outputs' unit when V's scale is beyond this many times it, or as small a part
+constexpr float kLift = 7.f;               // weights are held times 2^kLift: at most 2^15, fp16 ends at 2^16
 
 // eight codes as one matrix operand, exact
 __device__ __forceinline__ f16x8 widen8(uint32_t lo, uint32_t hi) {
@@ -107,12 +109,11 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
     const int split = blockIdx.x, b = blockIdx.z / a.h_kv, hk = blockIdx.z % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
     const int len = min(max(a.lens[b], 0), a.max_len);
     const int n_keys = min(len + a.R, a.max_len);
-    const int qi = blockIdx.y * 16 + i;
-    const int row = (qi < NQ ? qi : NQ - 1) % a.R, head = hk * group + (qi < NQ ? qi : NQ - 1) / a.R;
+    const int q0 = blockIdx.y * 16, qi = q0 + i;             // query row qi: head qi % group of the step's row qi / group
+    const int row = min(qi, NQ - 1) / group, head = hk * group + min(qi, NQ - 1) % group;
     QueryTile<DH> t;
     t.init(a, (int64_t)b * a.R + row, head, qi < NQ ? len + row : -1, g, scale_log2);
-    const int seen = min(len + chunk_last_row(blockIdx.y, 16, a.R, group) + 1, n_keys);    // no row of the block sees past it
-    const int all_see = len + (((int)blockIdx.y * 16) / a.R == (min((int)blockIdx.y * 16 + 16, NQ) - 1) / a.R ? ((int)blockIdx.y * 16) % a.R : 0) + 1;
+    const int seen = min(len + min(q0 + 15, NQ - 1) / group + 1, n_keys), all_see = len + q0 / group + 1;      // by some, by every row of the block
     const int n_blocks = (seen + kKv8Block - 1) / kKv8Block;
     const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
     const size_t cache_row = (size_t)b * a.h_kv + hk;
@@ -230,8 +231,8 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
             r += *reinterpret_cast<const f32x4 *>(&s_o[w][qc][d]) * f;
         }
         if (L != 0.f) r = r * (1.0f / L);                    // (a split none of whose keys the row sees: 0)
-        const int64_t m = (int64_t)b * a.R + q % a.R;
-        const int h = hk * group + q / a.R;
+        const int64_t m = (int64_t)b * a.R + q / group;
+        const int h = hk * group + q % group;
         if (a.splits == 1) {
             store_out4(a, m, h, d, r);
         } else {
@@ -240,6 +241,208 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
             if (d == 0) a.part_ml[at] = make_float2(M, L);
         }
     }
+}
+
+// Many query rows: four wavefronts of 32 rows each, on the 32 x 32 matrix instructions, walk the same keys.  The codes of 64 keys, 16 KB at
+// d_head 128, pass through LDS once for the block, in the order of the operands: a piece of 1 KB is what the 64 lanes read at
+// once, sixteen codes each, and becomes two operands.  Row x of K's tile t is key 32 t + 16 (x / 4 % 2) + 4 (x / 8) + x % 4, so that
+// a lane's scores, of keys 32 t + 16 h .. + 15 for lane half h, are in the order of V's pieces.
+template <int DH>
+__global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float scale_log2) {
+    constexpr int JT = DH / 32, PIECES = 4 * JT, MINE = PIECES / 4;        // K: 2 JT pieces [t][j], V: 2 JT [dt][w]
+    __shared__ u32x4 s_tile[2][PIECES][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 31, h = lane >> 5;
+    const int b = blockIdx.x / a.h_kv, hk = blockIdx.x % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
+    const int split = blockIdx.y, chunk = gridDim.z - 1 - blockIdx.z;      // the rows that see most go out first
+    const int len = min(max(a.lens[b], 0), a.max_len);
+    const int n_keys = min(len + a.R, a.max_len);
+    const int q0 = chunk * 128 + wave * 32, qi = q0 + i;
+    const int row = min(qi, NQ - 1) / group, head = hk * group + min(qi, NQ - 1) % group;
+    const int limit = qi < NQ ? len + row : -1;
+    // keys that some row of the block, some row and every row of the wavefront see
+    const int block_seen = min(len + min(chunk * 128 + 127, NQ - 1) / group + 1, n_keys);
+    const int wave_seen = q0 < NQ ? min(len + min(q0 + 31, NQ - 1) / group + 1, n_keys) : 0, all_see = len + q0 / group + 1;
+    const int n_blocks = (block_seen + kKv8Block - 1) / kKv8Block;
+    const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
+    const size_t cache_row = (size_t)b * a.h_kv + hk;
+    const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
+    const float *ks = a.k_scale + cache_row * (a.max_len / kKv8Block), *vs = a.v_scale + cache_row * (a.max_len / kKv8Block);
+
+    // a wavefront brings pieces of one kind: this lane's part of them lies these bytes into a block
+    const uint8_t *mine = wave < 2 ? K : V;
+    uint32_t src[MINE];
+#pragma unroll
+    for (int c = 0; c < MINE; ++c) {
+        const int x = (wave & 1) * MINE + c;
+        src[c] = wave < 2 ? (32 * (x / JT) + 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3)) * DH + 32 * (x % JT) + 16 * h
+                          : (32 * (x / 2) + i) * kKv8Block + 32 * (x % 2) + 16 * h;
+    }
+    u32x4 next[MINE];
+    auto load = [&](int kb) {
+        const uint8_t *block = mine + (size_t)kb * kKv8Block * DH;
+#pragma unroll
+        for (int c = 0; c < MINE; ++c) next[c] = *reinterpret_cast<const u32x4 *>(block + src[c]);
+    };
+    auto store = [&](int set) {
+#pragma unroll
+        for (int c = 0; c < MINE; ++c) s_tile[set][wave * MINE + c][lane] = next[c];
+    };
+    if (first < last) load(first);
+
+    f16x8 q[2 * JT];                                         // lane (query i, half h): entries 32 (s / 2) + 16 h + 8 (s % 2) .. + 7
+    float unit;
+    {
+        f32x8 v[2 * JT];
+        float top = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2 * JT; ++s) {
+            v[s] = load_q8(a, ((int64_t)b * a.R + row) * a.q_stride + head * DH + 32 * (s >> 1) + 16 * h + 8 * (s & 1));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[s][j]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const int e = min(max((int)(__float_as_uint(top) >> 23), 1), 253);
+        const float down = copysignf(__uint_as_float((uint32_t)(254 - e) << 23), scale_log2);
+        unit = fabsf(scale_log2) * __uint_as_float((uint32_t)e << 23);
+#pragma unroll
+        for (int s = 0; s < 2 * JT; ++s) q[s] = __builtin_bit_cast(f16x8, f32x8_to_f16x8(v[s] * down));
+    }
+    f32x16 o[JT];
+#pragma unroll
+    for (int dt = 0; dt < JT; ++dt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
+    float m = kFarBelow, l = 0.f, vref = 1.f;
+    if (first < last) store(0);
+    __syncthreads();
+
+    for (int kb = first; kb < last; ++kb) {
+        const int set = (kb - first) & 1;
+        if (kb + 1 < last) load(kb + 1);
+        if (kb * kKv8Block < wave_seen) {                    // (the same for the wavefront)
+            const u32x4 (*tile)[64] = s_tile[set];
+            const float k_scale = ks[kb], v_scale = vs[kb];
+            f32x16 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+#pragma unroll
+                for (int j = 0; j < JT; ++j) {
+                    const u32x4 w = tile[t * JT + j][lane];
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), q[2 * j], s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), q[2 * j + 1], s[t], 0, 0, 0);
+                }
+            }
+            float f = unit * k_scale;
+            const bool masked = kb * kKv8Block + kKv8Block > all_see;      // (the same for the wavefront)
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[t][r] = kb * kKv8Block + 32 * t + 16 * h + r > limit ? -INFINITY : s[t][r] * f;
+                f = 1.f;
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+            top *= f;
+            if (__ballot(top > m + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 32, kWave));
+                const float up = top > m + kSlack ? top : m, shrink = __builtin_amdgcn_exp2f(m - up);
+                m = up;
+                l *= shrink;
+#pragma unroll
+                for (int dt = 0; dt < JT; ++dt) o[dt] *= shrink;
+            }
+            // V's scale rides in the weights while it stays within 2^kSlackV of the outputs' unit, which else moves to it
+            float by = v_scale / vref;
+            if (!(by <= kSlackV && by >= 1.f / kSlackV)) {
+#pragma unroll
+                for (int dt = 0; dt < JT; ++dt) o[dt] *= 1.f / by;
+                vref = v_scale;
+                by = 1.f;
+            }
+            const float under = kLift - m + __builtin_amdgcn_logf(by);
+            float sum = 0.f;
+            f16x8 p[4];                                      // p[2 t + u]: keys 32 t + 16 h + 8 u .. + 7
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) {
+                    const f16x2 w = __builtin_convertvector((f32x2{__builtin_amdgcn_exp2f(fmaf(s[t][r], f, under)), __builtin_amdgcn_exp2f(fmaf(s[t][r + 1], f, under))}), f16x2);
+                    sum = __builtin_amdgcn_fdot2(w, f16x2{1, 1}, sum, false);
+                    p[2 * t + (r >> 3)][r & 7] = w[0];
+                    p[2 * t + (r >> 3)][(r & 7) + 1] = w[1];
+                }
+            l += sum / by;
+            uint32_t any = 0;
+            if (masked) {
+#pragma unroll
+                for (int x = 0; x < 2 * JT; ++x) {
+                    const u32x4 w = tile[2 * JT + x][lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) any |= nan_codes(w[e]);
+                }
+            }
+            if (__ballot(any != 0)) {                        // as in the direct kernel
+                f16x8 see[4];
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        see[2 * t + (r >> 3)][r & 7] = (_Float16)(kb * kKv8Block + 32 * t + 16 * h + r > limit ? 0.f : 1.f);
+#pragma unroll
+                for (int dt = 0; dt < JT; ++dt) {
+                    f32x16 hit;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) hit[r] = 0.f;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        u32x4 w = tile[2 * JT + 2 * dt + x][lane], n;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) { n[e] = nan_codes(w[e]); w[e] &= ~((n[e] >> 7) * 0xffu); }
+                        hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(n[0], n[1]), see[2 * x], hit, 0, 0, 0);
+                        hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(n[2], n[3]), see[2 * x + 1], hit, 0, 0, 0);
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), p[2 * x], o[dt], 0, 0, 0);
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), p[2 * x + 1], o[dt], 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (hit[r] > 0.f) o[dt][r] = __uint_as_float(0x7fc00000u);
+                }
+            } else {
+#pragma unroll
+                for (int dt = 0; dt < JT; ++dt)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const u32x4 w = tile[2 * JT + 2 * dt + x][lane];
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), p[2 * x], o[dt], 0, 0, 0);
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), p[2 * x + 1], o[dt], 0, 0, 0);
+                    }
+            }
+        }
+        if (kb + 1 < last) store(set ^ 1);                   // nobody reads that set any more: all are past the last barrier
+        __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32, kWave);
+    if (qi >= NQ) return;
+    const int64_t mrow = (int64_t)b * a.R + row;
+    const float inv = l != 0.f ? vref / l : 0.f;             // (a split none of whose keys the row sees: 0; a sum that is no number is not 0)
+    const size_t at = ((size_t)mrow * a.h_q + head) * a.splits + split;
+#pragma unroll
+    for (int dt = 0; dt < JT; ++dt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const int d = 32 * dt + 8 * x + 4 * h;
+            const f32x4 r = f32x4{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]} * inv;
+            if (a.splits == 1) store_out4(a, mrow, head, d, r);
+            else *reinterpret_cast<f32x4 *>(a.part_o + at * DH + d) = r;
+        }
+    if (a.splits > 1 && h == 0) a.part_ml[at] = make_float2(m, l);
 }
 
 // Joins the splits of a row and head, in their order: 64 / (d_h / 4) of them a wavefront, four entries a lane.
@@ -266,8 +469,11 @@ __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
 
 }  // namespace
 
+// Query rows of a KV head from which on they go 128 to a block
+inline bool use_wide(int NQ) { return NQ > 16; }
+
 int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
-    const int NQ = h_q / h_kv * R, chunks = (NQ + 15) / 16, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
+    const int NQ = h_q / h_kv * R, rows = use_wide(NQ) ? 128 : 16, chunks = (NQ + rows - 1) / rows, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
     long splits = 512 / ((long)B * h_kv * chunks);
     const int most = (blocks + 3) / 4;
     splits = splits > most ? most : splits;
@@ -276,7 +482,7 @@ int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound)
 
 int kv8_attn_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound, int *range) {
     const int blocks = (len_bound + kKv8Block - 1) / kKv8Block, splits = kv8_attn_max_splits(B, R, h_q, h_kv, d_h, len_bound);
-    const int r = (int)((blocks + splits - 1) / splits);
+    const int r = (blocks + splits - 1) / splits;
     if (range) *range = r;
     return (blocks + r - 1) / r;
 }
@@ -286,9 +492,15 @@ void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
     const int NQ = a.h_q / a.h_kv * a.R;
     {
         ScopedProf sp(PSD_KIND_ATTN, stream);
-        const dim3 grid(a.splits, (NQ + 15) / 16, a.B * a.h_kv);
-        if (a.d_h == 128) launch_kernel(attn8_direct_kernel<128>, grid, 256, 0, stream, a, scale_log2);
-        else launch_kernel(attn8_direct_kernel<64>, grid, 256, 0, stream, a, scale_log2);
+        if (use_wide(NQ)) {
+            const dim3 grid(a.B * a.h_kv, a.splits, (NQ + 127) / 128);
+            if (a.d_h == 128) launch_kernel(attn8_wide_kernel<128>, grid, 256, 0, stream, a, scale_log2);
+            else launch_kernel(attn8_wide_kernel<64>, grid, 256, 0, stream, a, scale_log2);
+        } else {
+            const dim3 grid(a.splits, (NQ + 15) / 16, a.B * a.h_kv);
+            if (a.d_h == 128) launch_kernel(attn8_direct_kernel<128>, grid, 256, 0, stream, a, scale_log2);
+            else launch_kernel(attn8_direct_kernel<64>, grid, 256, 0, stream, a, scale_log2);
+        }
     }
     if (a.splits > 1) {
         ScopedProf sp(PSD_KIND_ATTN_COMBINE, stream);
