@@ -41,28 +41,57 @@ __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7
 __device__ __forceinline__ f16x8 nan_flags(uint32_t lo, uint32_t hi) {
     return widen8((lo >> 7) * 0x38u, (hi >> 7) * 0x38u);     // 0x38 is 1.0
 }
+template <bool BF16>
 __device__ __forceinline__ f32x8 load_q8(const Kv8AttnArgs &a, int64_t at) {
-    if (a.q_bf16) {
-        const uint16_t *p = (const uint16_t *)a.q + at;
+    if constexpr (BF16) {
+        const u32x4 raw = *reinterpret_cast<const u32x4 *>((const uint16_t *)a.q + at);
         f32x8 v;
-        const u32x4 raw = *reinterpret_cast<const u32x4 *>(p);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (j & 1) ? __uint_as_float(raw[j >> 1] & 0xffff0000u) : __uint_as_float(raw[j >> 1] << 16);
         return v;
+    } else {
+        return load_f32x8((const float *)a.q + at);
     }
-    return load_f32x8((const float *)a.q + at);
 }
-// a finished result's entries d .. d + 3 of query head `head` of row m
-__device__ __forceinline__ void store_out4(const Kv8AttnArgs &a, int64_t m, int head, int d, f32x4 r) {
+// Where results go: the caller's bf16 rows, or what a forward's O projection reads; or, of one of several splits, to the combine kernel.
+// A build for each: the choice at every store made the epilogue several times the loop.
+enum { kOutBf16, kOutF32, kOutF16, kOutOp, kOutPart };
+// entries d .. d + 3 of query head `head` of row m
+template <int OUT>
+__device__ __forceinline__ void store_out4(const Kv8AttnArgs &a, int64_t m, int head, int split, int d, f32x4 r) {
     const int col = head * a.d_h + d;
-    if (a.out_bf16) *reinterpret_cast<uint2 *>(a.out_bf16 + m * a.out_stride + col) = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
     const int64_t at = m * a.h_q * a.d_h + col;
-    if (a.out) *reinterpret_cast<f32x4 *>(a.out + at) = r;
-    if (a.out16)
+    if constexpr (OUT == kOutBf16)
+        *reinterpret_cast<uint2 *>(a.out_bf16 + m * a.out_stride + col) = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
+    else if constexpr (OUT == kOutF32)
+        *reinterpret_cast<f32x4 *>(a.out + at) = r;
+    else if constexpr (OUT == kOutF16)
         *reinterpret_cast<uint2 *>(a.out16 + at) = make_uint2(f32_to_f16_bits(r[0]) | ((uint32_t)f32_to_f16_bits(r[1]) << 16),
                                                              f32_to_f16_bits(r[2]) | ((uint32_t)f32_to_f16_bits(r[3]) << 16));
-    if (a.out_op) op_store4(a.out_op, (int)m, col, a.op_folded, r);
+    else if constexpr (OUT == kOutOp)
+        op_store4(a.out_op, (int)m, col, a.op_folded, r);
+    else
+        *reinterpret_cast<f32x4 *>(a.part_o + ((m * a.h_q + head) * a.splits + split) * a.d_h + d) = r;
 }
+
+// The scales of 64 blocks, one a lane, and from there to the block that asks: scalar loads would come back among the LDS reads, in no
+// order, so that every wait for those became a wait for a scale's trip to memory (prompt of 2001 rows xx us against xx).
+struct Scales {
+    const float *k, *v;
+    int end, base;                // base: block of lane 0
+    float kw, vw;
+    __device__ __forceinline__ void fetch(int kb, int lane) {
+        base = kb;
+        const int at = min(kb + lane, end - 1);
+        kw = k[at];
+        vw = v[at];
+    }
+    __device__ __forceinline__ void at(int kb, int lane, float *k_scale, float *v_scale) {
+        if (kb >= base + kWave) fetch(kb, lane);
+        *k_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(kw), kb - base));
+        *v_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(vw), kb - base));
+    }
+};
 
 // One wavefront's part of a query tile of 16 rows: scores, weights and products over whole blocks of 64 keys.
 template <int DH>
@@ -74,6 +103,7 @@ struct QueryTile {
     float m, l;                   // reference; sum of this lane's weights, times 2^kLift
     f32x4 o[DT];                  // lane (query i, group g): entries 16 dt + 4 g .. + 3, in units of V's scale `vref`
 
+    template <bool QB>
     __device__ __forceinline__ void init(const Kv8AttnArgs &a, int64_t row, int head, int limit_, int g, float scale_log2) {
         limit = limit_;
         m = kFarBelow;
@@ -84,7 +114,7 @@ struct QueryTile {
         float top = 0.f;
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            v[s] = load_q8(a, row * a.q_stride + head * DH + 64 * (s >> 1) + 16 * g + 8 * (s & 1));
+            v[s] = load_q8<QB>(a, row * a.q_stride + head * DH + 64 * (s >> 1) + 16 * g + 8 * (s & 1));
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[s][j]));
         }
@@ -100,29 +130,33 @@ struct QueryTile {
 
 // Few query rows: the wavefronts of a block share its 16 query rows and take every fourth block of 64 keys each; their results are
 // joined in LDS, and those of a sequence's splits by the combine kernel.
-template <int DH>
+template <int DH, bool QB, int OUT>
 __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float scale_log2) {
     constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64;
     __shared__ float s_o[4][16][DH + 4];
     __shared__ float s_m[4][16], s_l[4][16];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
     const int split = blockIdx.x, b = blockIdx.z / a.h_kv, hk = blockIdx.z % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
     const int len = min(max(a.lens[b], 0), a.max_len);
     const int n_keys = min(len + a.R, a.max_len);
     const int q0 = blockIdx.y * 16, qi = q0 + i;             // query row qi: head qi % group of the step's row qi / group
     const int row = min(qi, NQ - 1) / group, head = hk * group + min(qi, NQ - 1) % group;
     QueryTile<DH> t;
-    t.init(a, (int64_t)b * a.R + row, head, qi < NQ ? len + row : -1, g, scale_log2);
+    t.template init<QB>(a, (int64_t)b * a.R + row, head, qi < NQ ? len + row : -1, g, scale_log2);
     const int seen = min(len + min(q0 + 15, NQ - 1) / group + 1, n_keys), all_see = len + q0 / group + 1;      // by some, by every row of the block
     const int n_blocks = (seen + kKv8Block - 1) / kKv8Block;
     const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
     const size_t cache_row = (size_t)b * a.h_kv + hk;
     const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
-    const float *ks = a.k_scale + cache_row * (a.max_len / kKv8Block), *vs = a.v_scale + cache_row * (a.max_len / kKv8Block);
+    const size_t scale_row = cache_row * (a.max_len / kKv8Block);
+    Scales scales{a.k_scale + scale_row, a.v_scale + scale_row, n_blocks, 0, 0.f, 0.f};
+    if (first < last) scales.fetch(first, lane);
     float vref = 1.f;
 
     for (int kb = first + wave; kb < last; kb += 4) {
         u32x4 kr[4][KL], vr[DT];
+        float k_scale, v_scale;
+        scales.at(kb, lane, &k_scale, &v_scale);             // (ahead of the loads: a wait for scales would be one for them)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -131,7 +165,6 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
             vr[dt] = *reinterpret_cast<const u32x4 *>(V + (size_t)kb * 64 * DH + (dt * 16 + i) * 64 + 16 * g);
-        const float k_scale = ks[kb], v_scale = vs[kb];
         f32x4 s[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) s[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -233,13 +266,8 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
         if (L != 0.f) r = r * (1.0f / L);                    // (a split none of whose keys the row sees: 0)
         const int64_t m = (int64_t)b * a.R + q / group;
         const int h = hk * group + q % group;
-        if (a.splits == 1) {
-            store_out4(a, m, h, d, r);
-        } else {
-            const size_t at = ((size_t)m * a.h_q + h) * a.splits + split;
-            *reinterpret_cast<f32x4 *>(a.part_o + at * DH + d) = r;
-            if (d == 0) a.part_ml[at] = make_float2(M, L);
-        }
+        store_out4<OUT>(a, m, h, split, d, r);
+        if (OUT == kOutPart && d == 0) a.part_ml[(m * a.h_q + h) * a.splits + split] = make_float2(M, L);
     }
 }
 
@@ -247,26 +275,31 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
 // d_head 128, pass through LDS once for the block, in the order of the operands: a piece of 1 KB is what the 64 lanes read at
 // once, sixteen codes each, and becomes two operands.  Row x of K's tile t is key 32 t + 16 (x / 4 % 2) + 4 (x / 8) + x % 4, so that
 // a lane's scores, of keys 32 t + 16 h .. + 15 for lane half h, are in the order of V's pieces.
-template <int DH>
+template <int DH, bool QB, int OUT>
 __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float scale_log2) {
     constexpr int JT = DH / 32, PIECES = 4 * JT, MINE = PIECES / 4;        // K: 2 JT pieces [t][j], V: 2 JT [dt][w]
     __shared__ u32x4 s_tile[2][PIECES][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 31, h = lane >> 5;
-    const int b = blockIdx.x / a.h_kv, hk = blockIdx.x % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
-    const int split = blockIdx.y, chunk = gridDim.z - 1 - blockIdx.z;      // the rows that see most go out first
+    // Blocks by how many keys they walk, most first, a head's chunk before the next chunk; those that fill the chip's second places
+    // the other way round, so that where all are resident at once a long one shares its CU with a short one.
+    uint32_t rank = blockIdx.x + gridDim.x * blockIdx.z;
+    if (rank >= 256u && gridDim.x * gridDim.z <= 512u) rank = 255u + gridDim.x * gridDim.z - rank;
+    const int bh = rank % gridDim.x, b = bh / a.h_kv, hk = bh % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
+    const int split = blockIdx.y, chunk = gridDim.z - 1 - rank / gridDim.x;
     const int len = min(max(a.lens[b], 0), a.max_len);
     const int n_keys = min(len + a.R, a.max_len);
     const int q0 = chunk * 128 + wave * 32, qi = q0 + i;
     const int row = min(qi, NQ - 1) / group, head = hk * group + min(qi, NQ - 1) % group;
     const int limit = qi < NQ ? len + row : -1;
-    // keys that some row of the block, some row and every row of the wavefront see
+    // keys that some row of the block, some row of the wavefront sees
     const int block_seen = min(len + min(chunk * 128 + 127, NQ - 1) / group + 1, n_keys);
-    const int wave_seen = q0 < NQ ? min(len + min(q0 + 31, NQ - 1) / group + 1, n_keys) : 0, all_see = len + q0 / group + 1;
+    const int wave_seen = q0 < NQ ? min(len + min(q0 + 31, NQ - 1) / group + 1, n_keys) : 0;
     const int n_blocks = (block_seen + kKv8Block - 1) / kKv8Block;
     const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
     const size_t cache_row = (size_t)b * a.h_kv + hk;
     const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
-    const float *ks = a.k_scale + cache_row * (a.max_len / kKv8Block), *vs = a.v_scale + cache_row * (a.max_len / kKv8Block);
+    const size_t scale_row = cache_row * (a.max_len / kKv8Block);
+    Scales scales{a.k_scale + scale_row, a.v_scale + scale_row, n_blocks, 0, 0.f, 0.f};
 
     // a wavefront brings pieces of one kind: this lane's part of them lies these bytes into a block
     const uint8_t *mine = wave < 2 ? K : V;
@@ -287,7 +320,10 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
 #pragma unroll
         for (int c = 0; c < MINE; ++c) s_tile[set][wave * MINE + c][lane] = next[c];
     };
-    if (first < last) load(first);
+    if (first < last) {
+        load(first);
+        scales.fetch(first, lane);
+    }
 
     f16x8 q[2 * JT];                                         // lane (query i, half h): entries 32 (s / 2) + 16 h + 8 (s % 2) .. + 7
     float unit;
@@ -296,7 +332,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
         float top = 0.f;
 #pragma unroll
         for (int s = 0; s < 2 * JT; ++s) {
-            v[s] = load_q8(a, ((int64_t)b * a.R + row) * a.q_stride + head * DH + 32 * (s >> 1) + 16 * h + 8 * (s & 1));
+            v[s] = load_q8<QB>(a, ((int64_t)b * a.R + row) * a.q_stride + head * DH + 32 * (s >> 1) + 16 * h + 8 * (s & 1));
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[s][j]));
         }
@@ -312,141 +348,151 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
     for (int dt = 0; dt < JT; ++dt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
-    float m = kFarBelow, l = 0.f, vref = 1.f;
+    float m = kFarBelow, l = 0.f, vref = 1.f, rvref = 1.f;
     if (first < last) store(0);
     __syncthreads();
 
-    for (int kb = first; kb < last; ++kb) {
-        const int set = (kb - first) & 1;
-        if (kb + 1 < last) load(kb + 1);
-        if (kb * kKv8Block < wave_seen) {                    // (the same for the wavefront)
-            const u32x4 (*tile)[64] = s_tile[set];
-            const float k_scale = ks[kb], v_scale = vs[kb];
-            f32x16 s[2];
+    auto step = [&](auto with_mask, int kb, int set, float k_scale, float v_scale) {
+        constexpr bool MASKED = decltype(with_mask)::value != 0;
+        const u32x4 (*tile)[64] = s_tile[set];
+        f32x16 s[2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
+            for (int r = 0; r < 16; ++r) s[t][r] = 0.f;
 #pragma unroll
-                for (int j = 0; j < JT; ++j) {
+        for (int j = 0; j < JT; ++j)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
                     const u32x4 w = tile[t * JT + j][lane];
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), q[2 * j], s[t], 0, 0, 0);
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), q[2 * j + 1], s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2 * u], w[2 * u + 1]), q[2 * j + u], s[t], 0, 0, 0);
                 }
-            }
-            float f = unit * k_scale;
-            const bool masked = kb * kKv8Block + kKv8Block > all_see;      // (the same for the wavefront)
-            if (masked) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[t][r] = kb * kKv8Block + 32 * t + 16 * h + r > limit ? -INFINITY : s[t][r] * f;
-                f = 1.f;
-            }
-            float top = s[0][0];
+        float f = unit * k_scale;
+        if constexpr (MASKED) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-            top *= f;
-            if (__ballot(top > m + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float up = top > m + kSlack ? top : m, shrink = __builtin_amdgcn_exp2f(m - up);
-                m = up;
-                l *= shrink;
+                for (int r = 0; r < 16; ++r) s[t][r] = kb * kKv8Block + 32 * t + 16 * h + r > limit ? -INFINITY : s[t][r] * f;
+            f = 1.f;
+        }
+        float top = s[0][0];
 #pragma unroll
-                for (int dt = 0; dt < JT; ++dt) o[dt] *= shrink;
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+        top *= f;
+        if (__ballot(top > m + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float up = top > m + kSlack ? top : m, shrink = __builtin_amdgcn_exp2f(m - up);
+            m = up;
+            l *= shrink;
+#pragma unroll
+            for (int dt = 0; dt < JT; ++dt) o[dt] *= shrink;
+        }
+        // V's scale rides in the weights while it stays within kSlackV of the outputs' unit, which else moves to it
+        float by = v_scale * rvref;
+        if (!(by <= kSlackV && by >= 1.f / kSlackV)) {
+            const float to = vref / v_scale;
+            vref = v_scale;
+            rvref = 1.f / v_scale;
+            by = 1.f;
+#pragma unroll
+            for (int dt = 0; dt < JT; ++dt) o[dt] *= to;
+        }
+        const float under = kLift - m + __builtin_amdgcn_logf(by);
+        float sum = 0.f;
+        f16x8 p[4];                                          // p[2 t + u]: keys 32 t + 16 h + 8 u .. + 7
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; r += 2) {
+                const f16x2 w = __builtin_convertvector((f32x2{__builtin_amdgcn_exp2f(fmaf(s[t][r], f, under)), __builtin_amdgcn_exp2f(fmaf(s[t][r + 1], f, under))}), f16x2);
+                sum = __builtin_amdgcn_fdot2(w, f16x2{1, 1}, sum, false);
+                p[2 * t + (r >> 3)][r & 7] = w[0];
+                p[2 * t + (r >> 3)][(r & 7) + 1] = w[1];
             }
-            // V's scale rides in the weights while it stays within 2^kSlackV of the outputs' unit, which else moves to it
-            float by = v_scale / vref;
-            if (!(by <= kSlackV && by >= 1.f / kSlackV)) {
-#pragma unroll
-                for (int dt = 0; dt < JT; ++dt) o[dt] *= 1.f / by;
-                vref = v_scale;
-                by = 1.f;
-            }
-            const float under = kLift - m + __builtin_amdgcn_logf(by);
-            float sum = 0.f;
-            f16x8 p[4];                                      // p[2 t + u]: keys 32 t + 16 h + 8 u .. + 7
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; r += 2) {
-                    const f16x2 w = __builtin_convertvector((f32x2{__builtin_amdgcn_exp2f(fmaf(s[t][r], f, under)), __builtin_amdgcn_exp2f(fmaf(s[t][r + 1], f, under))}), f16x2);
-                    sum = __builtin_amdgcn_fdot2(w, f16x2{1, 1}, sum, false);
-                    p[2 * t + (r >> 3)][r & 7] = w[0];
-                    p[2 * t + (r >> 3)][(r & 7) + 1] = w[1];
-                }
-            l += sum / by;
+        l += sum * __builtin_amdgcn_rcpf(by);
+        if constexpr (MASKED) {                              // what is no number where some row does not see it: as in the direct kernel
             uint32_t any = 0;
-            if (masked) {
 #pragma unroll
-                for (int x = 0; x < 2 * JT; ++x) {
-                    const u32x4 w = tile[2 * JT + x][lane];
+            for (int x = 0; x < 2 * JT; ++x) {
+                const u32x4 w = tile[2 * JT + x][lane];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) any |= nan_codes(w[e]);
-                }
+                for (int e = 0; e < 4; ++e) any |= nan_codes(w[e]);
             }
-            if (__ballot(any != 0)) {                        // as in the direct kernel
-                f16x8 see[4];
+            const bool bad = __ballot(any != 0) != 0;
+            f16x8 see[4];
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        see[2 * t + (r >> 3)][r & 7] = (_Float16)(kb * kKv8Block + 32 * t + 16 * h + r > limit ? 0.f : 1.f);
+                for (int r = 0; r < 16; ++r)
+                    see[2 * t + (r >> 3)][r & 7] = (_Float16)(kb * kKv8Block + 32 * t + 16 * h + r > limit ? 0.f : 1.f);
 #pragma unroll
-                for (int dt = 0; dt < JT; ++dt) {
-                    f32x16 hit;
+            for (int dt = 0; dt < JT; ++dt)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) hit[r] = 0.f;
+                for (int x = 0; x < 2; ++x) {
+                    u32x4 w = tile[2 * JT + 2 * dt + x][lane];
+                    if (bad) {
+                        f32x16 hit;
+                        u32x4 n;
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        u32x4 w = tile[2 * JT + 2 * dt + x][lane], n;
+                        for (int r = 0; r < 16; ++r) hit[r] = 0.f;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) { n[e] = nan_codes(w[e]); w[e] &= ~((n[e] >> 7) * 0xffu); }
                         hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(n[0], n[1]), see[2 * x], hit, 0, 0, 0);
                         hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(n[2], n[3]), see[2 * x + 1], hit, 0, 0, 0);
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), p[2 * x], o[dt], 0, 0, 0);
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), p[2 * x + 1], o[dt], 0, 0, 0);
-                    }
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (hit[r] > 0.f) o[dt][r] = __uint_as_float(0x7fc00000u);
+                        for (int r = 0; r < 16; ++r)
+                            if (hit[r] > 0.f) o[dt][r] = __uint_as_float(0x7fc00000u);
+                    }
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), p[2 * x], o[dt], 0, 0, 0);
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), p[2 * x + 1], o[dt], 0, 0, 0);
                 }
-            } else {
+        } else {
 #pragma unroll
-                for (int dt = 0; dt < JT; ++dt)
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int dt = 0; dt < JT; ++dt) {
                         const u32x4 w = tile[2 * JT + 2 * dt + x][lane];
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), p[2 * x], o[dt], 0, 0, 0);
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), p[2 * x + 1], o[dt], 0, 0, 0);
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2 * u], w[2 * u + 1]), p[2 * x + u], o[dt], 0, 0, 0);
                     }
-            }
         }
-        if (kb + 1 < last) store(set ^ 1);                   // nobody reads that set any more: all are past the last barrier
-        __syncthreads();
-    }
+    };
+    // blocks of keys that every row of the block sees, then those that need the mask
+    const int whole = min(last, (len + chunk * 128 / group + 1) / kKv8Block);
+    int kb = first, set = 0;
+    auto walk = [&](auto with_mask, int end) {
+        for (; kb < end; ++kb, set ^= 1) {
+            float k_scale, v_scale;
+            scales.at(kb, lane, &k_scale, &v_scale);         // (ahead of the loads: a wait for scales would be one for them)
+            load(kb + 1 < last ? kb + 1 : kb);
+            if (decltype(with_mask)::value == 0 || kb * kKv8Block < wave_seen) step(with_mask, kb, set, k_scale, v_scale);       // (the same for the wavefront)
+            store(set ^ 1);                                  // nobody reads that set any more: all are past the last barrier
+            __syncthreads();
+        }
+    };
+    walk(Int<0>{}, whole);
+    walk(Int<1>{}, last);
 
     l += __shfl_xor(l, 32, kWave);
     if (qi >= NQ) return;
     const int64_t mrow = (int64_t)b * a.R + row;
     const float inv = l != 0.f ? vref / l : 0.f;             // (a split none of whose keys the row sees: 0; a sum that is no number is not 0)
-    const size_t at = ((size_t)mrow * a.h_q + head) * a.splits + split;
 #pragma unroll
     for (int dt = 0; dt < JT; ++dt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            const int d = 32 * dt + 8 * x + 4 * h;
-            const f32x4 r = f32x4{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]} * inv;
-            if (a.splits == 1) store_out4(a, mrow, head, d, r);
-            else *reinterpret_cast<f32x4 *>(a.part_o + at * DH + d) = r;
-        }
-    if (a.splits > 1 && h == 0) a.part_ml[at] = make_float2(m, l);
+        for (int x = 0; x < 4; ++x)
+            store_out4<OUT>(a, mrow, head, split, 32 * dt + 8 * x + 4 * h,
+                            f32x4{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]} * inv);
+    if (OUT == kOutPart && h == 0) a.part_ml[(mrow * a.h_q + head) * a.splits + split] = make_float2(m, l);
 }
 
 // Joins the splits of a row and head, in their order: 64 / (d_h / 4) of them a wavefront, four entries a lane.
-template <int DH>
+template <int DH, int OUT>
 __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
     constexpr int kLanes = DH / 4, kRows = 256 / kLanes;
     const int64_t rh = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
@@ -464,7 +510,7 @@ __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
         L += w;
         r += *reinterpret_cast<const f32x4 *>(o + (size_t)s * DH) * w;
     }
-    store_out4(a, rh / a.h_q, (int)(rh % a.h_q), d, r * (1.0f / L));
+    store_out4<OUT>(a, rh / a.h_q, (int)(rh % a.h_q), 0, d, r * (1.0f / L));
 }
 
 }  // namespace
@@ -490,24 +536,46 @@ int kv8_attn_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound, int
 void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
     const float scale_log2 = 1.4426950408889634f * a.scale;
     const int NQ = a.h_q / a.h_kv * a.R;
+    auto by_head = [&](auto kernels) {
+        if (a.d_h == 128) kernels(Int<128>{});
+        else kernels(Int<64>{});
+    };
+    auto by_out = [&](auto kernels) {
+        if (a.out_bf16) kernels(Int<kOutBf16>{});
+        else if (a.out) kernels(Int<kOutF32>{});
+        else if (a.out16) kernels(Int<kOutF16>{});
+        else kernels(Int<kOutOp>{});
+    };
     {
         ScopedProf sp(PSD_KIND_ATTN, stream);
-        if (use_wide(NQ)) {
-            const dim3 grid(a.B * a.h_kv, a.splits, (NQ + 127) / 128);
-            if (a.d_h == 128) launch_kernel(attn8_wide_kernel<128>, grid, 256, 0, stream, a, scale_log2);
-            else launch_kernel(attn8_wide_kernel<64>, grid, 256, 0, stream, a, scale_log2);
-        } else {
-            const dim3 grid(a.splits, (NQ + 15) / 16, a.B * a.h_kv);
-            if (a.d_h == 128) launch_kernel(attn8_direct_kernel<128>, grid, 256, 0, stream, a, scale_log2);
-            else launch_kernel(attn8_direct_kernel<64>, grid, 256, 0, stream, a, scale_log2);
-        }
+        auto go = [&](auto dh, auto qb, auto out) {
+            constexpr int DH = decltype(dh)::value, OUT = decltype(out)::value;
+            constexpr bool QB = decltype(qb)::value != 0;
+            if (use_wide(NQ))
+                launch_kernel(attn8_wide_kernel<DH, QB, OUT>, dim3(a.B * a.h_kv, a.splits, (NQ + 127) / 128), 256, 0, stream, a, scale_log2);
+            else
+                launch_kernel(attn8_direct_kernel<DH, QB, OUT>, dim3(a.splits, (NQ + 15) / 16, a.B * a.h_kv), 256, 0, stream, a, scale_log2);
+        };
+        by_head([&](auto dh) {
+            if (a.splits > 1) {
+                if (a.q_bf16) go(dh, Int<1>{}, Int<kOutPart>{});
+                else go(dh, Int<0>{}, Int<kOutPart>{});
+            } else if (a.q_bf16) {
+                go(dh, Int<1>{}, Int<kOutBf16>{});           // (bf16 queries are the caller's, and so is the output)
+            } else {
+                by_out([&](auto out) {
+                    if constexpr (decltype(out)::value != kOutBf16) go(dh, Int<0>{}, out);
+                });
+            }
+        });
     }
     if (a.splits > 1) {
         ScopedProf sp(PSD_KIND_ATTN_COMBINE, stream);
         const int64_t rows = (int64_t)a.B * a.R * a.h_q, per = 256 / (a.d_h / 4);
         const unsigned grid = (unsigned)((rows + per - 1) / per);
-        if (a.d_h == 128) launch_kernel(attn8_combine_kernel<128>, grid, 256, 0, stream, a);
-        else launch_kernel(attn8_combine_kernel<64>, grid, 256, 0, stream, a);
+        by_head([&](auto dh) {
+            by_out([&](auto out) { launch_kernel(attn8_combine_kernel<decltype(dh)::value, decltype(out)::value>, grid, 256, 0, stream, a); });
+        });
     }
 }
 
