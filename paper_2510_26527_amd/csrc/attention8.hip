@@ -279,6 +279,7 @@ template <int DH, bool QB, int OUT>
 __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float scale_log2) {
     constexpr int JT = DH / 32, PIECES = 4 * JT, MINE = PIECES / 4;        // K: 2 JT pieces [t][j], V: 2 JT [dt][w]
     __shared__ u32x4 s_tile[2][PIECES][64];
+    __shared__ int s_nan[2][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 31, h = lane >> 5;
     // Blocks by how many keys they walk, most first, a head's chunk before the next chunk; those that fill the chip's second places
     // the other way round, so that where all are resident at once a long one shares its CU with a short one.
@@ -296,6 +297,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
     const int wave_seen = q0 < NQ ? min(len + min(q0 + 31, NQ - 1) / group + 1, n_keys) : 0;
     const int n_blocks = (block_seen + kKv8Block - 1) / kKv8Block;
     const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
+    const int whole = min(last, (len + chunk * 128 / group + 1) / kKv8Block);              // blocks of keys below that every row of the block sees
     const size_t cache_row = (size_t)b * a.h_kv + hk;
     const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
     const size_t scale_row = cache_row * (a.max_len / kKv8Block);
@@ -316,7 +318,22 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
 #pragma unroll
         for (int c = 0; c < MINE; ++c) next[c] = *reinterpret_cast<const u32x4 *>(block + src[c]);
     };
-    auto store = [&](int set) {
+    // look: a block that needs the mask.  A position that some row does not see may hold anything: what is no number among V's entries
+    // must not reach the product, where a weight of 0 would not keep it out.
+    auto store = [&](int set, bool look) {
+        if (look && wave >= 2) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int c = 0; c < MINE; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t n = nan_codes(next[c][e]);
+                    any |= n;
+                    next[c][e] &= ~((n >> 7) * 0xffu);
+                }
+            const bool found = __ballot(any != 0) != 0;
+            if (lane == 0) s_nan[set][wave - 2] = found;
+        }
 #pragma unroll
         for (int c = 0; c < MINE; ++c) s_tile[set][wave * MINE + c][lane] = next[c];
     };
@@ -349,11 +366,12 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     float m = kFarBelow, l = 0.f, vref = 1.f, rvref = 1.f;
-    if (first < last) store(0);
+    if (first < last) store(0, first >= whole);
     __syncthreads();
 
     auto step = [&](auto with_mask, int kb, int set, float k_scale, float v_scale) {
         constexpr bool MASKED = decltype(with_mask)::value != 0;
+        const int room = limit - (kb * kKv8Block + 16 * h);  // of this lane's keys 32 t + r those up to there are seen
         const u32x4 (*tile)[64] = s_tile[set];
         f32x16 s[2];
 #pragma unroll
@@ -374,7 +392,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[t][r] = kb * kKv8Block + 32 * t + 16 * h + r > limit ? -INFINITY : s[t][r] * f;
+                for (int r = 0; r < 16; ++r) s[t][r] = 32 * t + r > room ? -INFINITY : s[t][r] * f;
             f = 1.f;
         }
         float top = s[0][0];
@@ -414,64 +432,54 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
                 p[2 * t + (r >> 3)][(r & 7) + 1] = w[1];
             }
         l += sum * __builtin_amdgcn_rcpf(by);
-        if constexpr (MASKED) {                              // what is no number where some row does not see it: as in the direct kernel
-            uint32_t any = 0;
 #pragma unroll
-            for (int x = 0; x < 2 * JT; ++x) {
-                const u32x4 w = tile[2 * JT + x][lane];
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) any |= nan_codes(w[e]);
-            }
-            const bool bad = __ballot(any != 0) != 0;
-            f16x8 see[4];
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    see[2 * t + (r >> 3)][r & 7] = (_Float16)(kb * kKv8Block + 32 * t + 16 * h + r > limit ? 0.f : 1.f);
-#pragma unroll
-            for (int dt = 0; dt < JT; ++dt)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    u32x4 w = tile[2 * JT + 2 * dt + x][lane];
-                    if (bad) {
-                        f32x16 hit;
-                        u32x4 n;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) hit[r] = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) { n[e] = nan_codes(w[e]); w[e] &= ~((n[e] >> 7) * 0xffu); }
-                        hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(n[0], n[1]), see[2 * x], hit, 0, 0, 0);
-                        hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(n[2], n[3]), see[2 * x + 1], hit, 0, 0, 0);
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (hit[r] > 0.f) o[dt][r] = __uint_as_float(0x7fc00000u);
-                    }
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[0], w[1]), p[2 * x], o[dt], 0, 0, 0);
-                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2], w[3]), p[2 * x + 1], o[dt], 0, 0, 0);
+                for (int dt = 0; dt < JT; ++dt) {
+                    const u32x4 w = tile[2 * JT + 2 * dt + x][lane];
+                    o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2 * u], w[2 * u + 1]), p[2 * x + u], o[dt], 0, 0, 0);
                 }
-        } else {
+    };
+    // V's entries that are no number in a block that needs the mask (they are zeros in LDS): rows that see one get it
+    auto holes = [&](int kb) {
+        const int room = limit - (kb * kKv8Block + 16 * h);
+        f16x8 see[4];
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+            for (int r = 0; r < 16; ++r) see[2 * t + (r >> 3)][r & 7] = (_Float16)(32 * t + r > room ? 0.f : 1.f);
 #pragma unroll
-                    for (int dt = 0; dt < JT; ++dt) {
-                        const u32x4 w = tile[2 * JT + 2 * dt + x][lane];
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2 * u], w[2 * u + 1]), p[2 * x + u], o[dt], 0, 0, 0);
-                    }
+        for (int dt = 0; dt < JT; ++dt) {
+            f32x16 hit;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) hit[r] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const u32x4 w = *reinterpret_cast<const u32x4 *>(V + (size_t)kb * kKv8Block * DH + (32 * dt + i) * kKv8Block + 32 * x + 16 * h);
+                hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(nan_codes(w[0]), nan_codes(w[1])), see[2 * x], hit, 0, 0, 0);
+                hit = __builtin_amdgcn_mfma_f32_32x32x16_f16(nan_flags(nan_codes(w[2]), nan_codes(w[3])), see[2 * x + 1], hit, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (hit[r] > 0.f) o[dt][r] = __uint_as_float(0x7fc00000u);
         }
     };
     // blocks of keys that every row of the block sees, then those that need the mask
-    const int whole = min(last, (len + chunk * 128 / group + 1) / kKv8Block);
     int kb = first, set = 0;
     auto walk = [&](auto with_mask, int end) {
         for (; kb < end; ++kb, set ^= 1) {
             float k_scale, v_scale;
             scales.at(kb, lane, &k_scale, &v_scale);         // (ahead of the loads: a wait for scales would be one for them)
             load(kb + 1 < last ? kb + 1 : kb);
-            if (decltype(with_mask)::value == 0 || kb * kKv8Block < wave_seen) step(with_mask, kb, set, k_scale, v_scale);       // (the same for the wavefront)
-            store(set ^ 1);                                  // nobody reads that set any more: all are past the last barrier
+            if constexpr (decltype(with_mask)::value == 0) {
+                step(with_mask, kb, set, k_scale, v_scale);
+            } else if (kb * kKv8Block < wave_seen) {         // (the same for the wavefront)
+                if (s_nan[set][0] | s_nan[set][1]) holes(kb);
+                step(with_mask, kb, set, k_scale, v_scale);
+            }
+            store(set ^ 1, kb + 1 >= whole);                                  // nobody reads that set any more: all are past the last barrier
             __syncthreads();
         }
     };
