@@ -129,9 +129,9 @@ def _ptr(t):
 
 
 def _stream_ptr(stream):
-    if stream is None:
+    if stream is None:                       # the current device's current stream, without a Stream object (2.6 us of a call)
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -37,9 +37,11 @@ __device__ __forceinline__ f16x8 widen8(uint32_t lo, uint32_t hi) {
 }
 // bytes of w that hold e4m3's NaN, as 0x80
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// w with zeros there
+__device__ __forceinline__ uint32_t without_nan(uint32_t w, uint32_t n) { return w & ~((n << 1) - (n >> 7)); }
 // ... and 0x80 bytes as fp16 ones
 __device__ __forceinline__ f16x8 nan_flags(uint32_t lo, uint32_t hi) {
-    return widen8((lo >> 7) * 0x38u, (hi >> 7) * 0x38u);     // 0x38 is 1.0
+    return widen8((lo >> 2) + (lo >> 3) + (lo >> 4), (hi >> 2) + (hi >> 3) + (hi >> 4));      // 0x38 is 1.0
 }
 template <bool BF16>
 __device__ __forceinline__ f32x8 load_q8(const Kv8AttnArgs &a, int64_t at) {
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
                     f32x4 hit{0.f, 0.f, 0.f, 0.f};
                     uint32_t n[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { n[e] = nan_codes(vr[dt][e]); vr[dt][e] &= ~((n[e] >> 7) * 0xffu); }
+                    for (int e = 0; e < 4; ++e) { n[e] = nan_codes(vr[dt][e]); vr[dt][e] = without_nan(vr[dt][e], n[e]); }
                     hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(nan_flags(n[0], n[1]), see[0], hit, 0, 0, 0);
                     hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(nan_flags(n[2], n[3]), see[1], hit, 0, 0, 0);
 #pragma unroll
@@ -329,7 +331,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t n = nan_codes(next[c][e]);
                     any |= n;
-                    next[c][e] &= ~((n >> 7) * 0xffu);
+                    next[c][e] = without_nan(next[c][e], n);
                 }
             const bool found = __ballot(any != 0) != 0;
             if (lane == 0) s_nan[set][wave - 2] = found;

@@ -117,27 +117,34 @@ class KVCache:
             self.handle = None
 
 
-def _current(t):
+_CODE = {torch.float32: psd.PSD_F32, torch.bfloat16: psd.PSD_BF16}
+
+
+def _current(*tensors):
     """The library enqueues on the current device: a tensor of another one is the caller's mistake."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensor on {t.device}, the current device is {torch.cuda.current_device()}")
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t.get_device() != here:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
 
 
-def _row_stride(t, rows):
+def _row_stride(t):
     """Elements between the rows of t [..., heads, d], whose heads are dense within a row, and rows evenly apart."""
-    if t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1]):
+    shape, strides = t.shape, t.stride()
+    width = shape[-2] * shape[-1]
+    if t.is_contiguous():
+        return width
+    if strides[-1] != 1 or (shape[-2] > 1 and strides[-2] != shape[-1]):
         raise ValueError("a row's heads have to lie side by side")
     stride, span = None, 1
-    for n, st in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
-        if n > 1:
+    for k in range(len(shape) - 3, -1, -1):
+        if shape[k] > 1:
             if stride is None:
-                stride = st
-            elif st != stride * span:
+                stride = strides[k]
+            elif strides[k] != stride * span:
                 raise ValueError("rows have to be evenly apart")
-            span *= n
-    if span != rows:
-        raise ValueError(f"{rows} rows expected, got {tuple(t.shape[:-2])}")
-    return t.shape[-2] * t.shape[-1] if stride is None else stride
+            span *= shape[k]
+    return width if stride is None else stride
 
 
 class Rope:
@@ -158,27 +165,23 @@ class Rope:
 
     def rotate(self, x, positions, out=None, stream=None):
         """x [..., heads, d_head] (fp32 or bf16), positions int32 of its leading shape -> a new tensor, or `out` (which may be x)."""
-        _current(x)
-        rows = positions.numel()
-        if x.shape[:-2] != positions.shape or x.shape[-1] != self.d_head or positions.dtype != torch.int32 or not positions.is_contiguous():
+        shape = x.shape
+        if shape[:-2] != positions.shape or shape[-1] != self.d_head or positions.dtype != torch.int32 or not positions.is_contiguous():
             raise ValueError("x [..., heads, d_head] with contiguous int32 positions [...] expected")
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        elif out.shape != x.shape or out.dtype != x.dtype:
+            out = torch.empty_like(x)
+        elif out.shape != shape or out.dtype != x.dtype:
             raise ValueError("out has another shape or type than x")
-        if positions.device != x.device or out.device != x.device:
-            raise ValueError("tensors on different devices")
+        _current(x, positions, out)
+        rows = positions.numel()
         if rows:
-            psd.psd_rope_rotate(self.handle, x, out, positions, rows, x.shape[-2], psd.dtype_code(x.dtype), _row_stride(x, rows),
-                                _row_stride(out, rows), stream)
+            psd.psd_rope_rotate(self.handle, x, out, positions, rows, shape[-2], _CODE[x.dtype], _row_stride(x), _row_stride(out), stream)
         return out
 
     def close(self):
         if self.handle is not None:
             psd.psd_rope_destroy(self.handle)
             self.handle = None
-
-    __del__ = close
 
 
 class KVCache8:
@@ -248,25 +251,26 @@ class KV8Layer:
     def append(self, q, k, v, rope=None, len_upper_bound=None, q_out=None, stream=None):
         """Rows q [B, n_new, h_q, d_h] (or None), k and v [B, n_new, h_kv, d_h], all fp32 or all bf16, at positions lens[b] ..: rotated
         by `rope` and quantised into the cache -> the rotated queries.  len_upper_bound: a bound of lens[b] + n_new."""
-        _current(k)
-        B, n, h, d = k.shape
-        if (B, h, d) != (self.view.batch, self.view.n_kv_heads, self.view.d_head) or v.shape != k.shape or v.dtype != k.dtype:
+        shape, view = k.shape, self.view
+        B, n, h, d = shape
+        if B != view.batch or h != view.n_kv_heads or d != view.d_head or v.shape != shape or v.dtype != k.dtype:
             raise ValueError("k and v are [B, n_new, n_kv_heads, d_head] of one type")
-        rows, q_stride, out_stride, h_q = B * n, 0, 0, h
-        if q is not None:
-            if q.shape[:2] != k.shape[:2] or q.shape[3] != d or q.dtype != k.dtype:
+        q_stride, out_stride, h_q = 0, 0, h
+        if q is None:
+            q_out = None
+            _current(k, v, self.k)
+        else:
+            h_q = q.shape[2]
+            if q.shape != (B, n, h_q, d) or q.dtype != k.dtype:
                 raise ValueError("q is [B, n_new, n_q_heads, d_head] of k's type")
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                q_out = torch.empty_like(q)
             elif q_out.shape != q.shape or q_out.dtype != q.dtype:
                 raise ValueError("q_out has another shape or type than q")
-            h_q, q_stride, out_stride = q.shape[2], _row_stride(q, rows), _row_stride(q_out, rows)
-        for t in (q, v, q_out, self.k):
-            if t is not None and t.device != k.device:
-                raise ValueError("tensors on different devices")
-        psd.psd_kv8_append(self.view, None if rope is None else rope.handle, q, k, v, q_out, n, h_q, psd.dtype_code(k.dtype), q_stride,
-                           _row_stride(k, rows), _row_stride(v, rows), out_stride,
-                           self.view.max_len if len_upper_bound is None else len_upper_bound, stream)
+            _current(k, v, self.k, q, q_out)
+            q_stride, out_stride = _row_stride(q), _row_stride(q_out)
+        psd.psd_kv8_append(view, None if rope is None else rope.handle, q, k, v, q_out, n, h_q, _CODE[k.dtype], q_stride,
+                           _row_stride(k), _row_stride(v), out_stride, view.max_len if len_upper_bound is None else len_upper_bound, stream)
         return q_out
 
 
@@ -279,23 +283,26 @@ class KV8Attention:
     def __call__(self, cache: KV8Layer, q, scale=0.0, len_upper_bound=None, out=None, stream=None):
         """q bf16 [B, n_new, h_q, d_h], the rows just appended to `cache` -> bf16 of the same shape; scale 0: 1 / sqrt(d_h).
         len_upper_bound: a bound of lens[b] + n_new."""
-        _current(q)
-        B, n, h_q, d = q.shape
         view = cache.view
-        if (B, d) != (view.batch, view.d_head) or q.dtype != torch.bfloat16:
+        B, n, h_q, d = q.shape
+        if B != view.batch or d != view.d_head or q.dtype != torch.bfloat16:
             raise ValueError("q is bf16 [B, n_new, n_q_heads, d_head]")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            out = torch.empty_like(q)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out has another shape or type than q")
-        if cache.k.device != q.device or out.device != q.device:
-            raise ValueError("tensors on different devices")
+        _current(q, cache.k, out)
         bound = view.max_len if len_upper_bound is None else len_upper_bound
-        need = psd.psd_kv8_attention_workspace_bytes(B, n, h_q, view.n_kv_heads, d, bound)
-        if need and (self._ws is None or self._ws.numel() < need or self._ws.device != q.device):
-            self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
-        psd.psd_kv8_attention(view, q, out, n, h_q, scale, _row_stride(q, B * n), _row_stride(out, B * n), bound, self._ws, stream)
-        return out
+        q_stride, out_stride = _row_stride(q), _row_stride(out)
+        for grown in (False, True):
+            try:
+                psd.psd_kv8_attention(view, q, out, n, h_q, scale, q_stride, out_stride, bound, self._ws, stream)
+                return out
+            except psd.PsdError as e:                        # too small a workspace so far: nothing was enqueued
+                if grown or e.status != psd.PSD_ERR_WORKSPACE:
+                    raise
+                need = psd.psd_kv8_attention_workspace_bytes(B, n, h_q, view.n_kv_heads, d, bound)
+                self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
 
 
 def forward(model: Model, kv: KVCache, tokens, n_logit_rows=None, logits_out=None, stream=None):
