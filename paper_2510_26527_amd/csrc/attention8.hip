@@ -29,6 +29,16 @@ constexpr float kSlack = 5.f;              // the reference moves when a score i
 constexpr float kSlackV = 8.f;             // ... and the outputs' unit when V's scale is beyond this many times it, or as small a part
 constexpr float kLift = 7.f;               // weights are held times 2^kLift: at most 2^15, fp16 ends at 2^16
 
+// Whether a reference is so large (2^8 powers of two) that an exponent must not be put together from it by fma: score * unit would go in
+// unrounded where the reference was rounded, and what is added to the reference would be lost in it.  The difference is then taken first.
+__device__ __forceinline__ bool is_large(float m) { return fabsf(m) > 256.f && m != kFarBelow; }
+
+__device__ __forceinline__ float above(float score, float unit, float m) {
+#pragma clang fp contract(off)
+    const float x = score * unit;
+    return x - m;
+}
+
 // eight codes as one matrix operand, exact
 __device__ __forceinline__ f16x8 widen8(uint32_t lo, uint32_t hi) {
     const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
@@ -123,8 +133,8 @@ struct QueryTile {
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
         const int e = min(max((int)(__float_as_uint(top) >> 23), 1), 253);                 // 2^(e - 127) <= top
-        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
-        unit = scale_log2 * __uint_as_float((uint32_t)e << 23);
+        const float down = copysignf(__uint_as_float((uint32_t)(254 - e) << 23), scale_log2);             // (unit stays positive)
+        unit = fabsf(scale_log2) * __uint_as_float((uint32_t)e << 23);
 #pragma unroll
         for (int s = 0; s < KS; ++s) q[s] = __builtin_bit_cast(f16x8, f32x8_to_f16x8(v[s] * down));
     }
@@ -133,7 +143,7 @@ struct QueryTile {
 // Few query rows: the wavefronts of a block share its 16 query rows and take every fourth block of 64 keys each; their results are
 // joined in LDS, and those of a sequence's splits by the combine kernel.
 template <int DH, bool QB, int OUT>
-__global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float scale_log2) {
+__global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, float scale_log2) {
     constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64;
     __shared__ float s_o[4][16][DH + 4];
     __shared__ float s_m[4][16], s_l[4][16];
@@ -153,63 +163,30 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
     const size_t scale_row = cache_row * (a.max_len / kKv8Block);
     Scales scales{a.k_scale + scale_row, a.v_scale + scale_row, n_blocks, 0, 0.f, 0.f};
     if (first < last) scales.fetch(first, lane);
-    float vref = 1.f;
+    float vref = 1.f, rvref = 1.f;
+    bool large = false;
 
-    for (int kb = first + wave; kb < last; kb += 4) {
-        u32x4 kr[4][KL], vr[DT];
-        float k_scale, v_scale;
-        scales.at(kb, lane, &k_scale, &v_scale);             // (ahead of the loads: a wait for scales would be one for them)
+    // The next block's codes are on their way while this one is worked on: at d_head 64 in registers of their own, at 128, where a block's
+    // fill 64 and a second set of them spills, in the present one's, K's from the scores on and V's from the product on.
+    constexpr int SETS = DH == 64 ? 2 : 1;
+    u32x4 kr[SETS][4][KL], vr[SETS][DT];
+    auto load_k = [&](auto at, int kb) {
+        const uint8_t *p = K + (size_t)kb * kKv8Block * DH;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
             for (int j = 0; j < KL; ++j)
-                kr[c][j] = *reinterpret_cast<const u32x4 *>(K + ((size_t)kb * 64 + 16 * (i >> 2) + 4 * c + (i & 3)) * DH + 64 * j + 16 * g);
+                kr[decltype(at)::value][c][j] = *reinterpret_cast<const u32x4 *>(p + (16 * (i >> 2) + 4 * c + (i & 3)) * DH + 64 * j + 16 * g);
+    };
+    auto load_v = [&](auto at, int kb) {
+        const uint8_t *p = V + (size_t)kb * kKv8Block * DH;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-            vr[dt] = *reinterpret_cast<const u32x4 *>(V + (size_t)kb * 64 * DH + (dt * 16 + i) * 64 + 16 * g);
-        f32x4 s[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) s[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < KS; ++e)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                s[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(kr[c][e >> 1][2 * (e & 1)], kr[c][e >> 1][2 * (e & 1) + 1]), t.q[e], s[c], 0, 0, 0);
-        const float f = t.unit * k_scale;
-        float top = -INFINITY;
-        const bool masked = kb * 64 + 64 > all_see;          // (the same for the whole block)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[c][e] *= f;
-                if (masked && kb * 64 + 16 * g + 4 * c + e > t.limit) s[c][e] = -INFINITY;
-                top = fmaxf(top, s[c][e]);
-            }
-        if (__ballot(top > t.m + kSlack)) {
-            top = fmaxf(top, __shfl_xor(top, 16, kWave));
-            top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float m = top > t.m + kSlack ? top : t.m, shrink = __builtin_amdgcn_exp2f(t.m - m);
-            t.m = m;
-            t.l *= shrink;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) t.o[dt] *= shrink;
-        }
-        if (v_scale != vref) {
-            const float to = vref / v_scale;
-            vref = v_scale;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) t.o[dt] *= to;
-        }
-        f16x8 p[2];
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float w = __builtin_amdgcn_exp2f(s[c][e] - (t.m - kLift));
-                t.l += w;
-                p[c >> 1][4 * (c & 1) + e] = (_Float16)w;
-            }
+        for (int dt = 0; dt < DT; ++dt) vr[decltype(at)::value][dt] = *reinterpret_cast<const u32x4 *>(p + (dt * 16 + i) * kKv8Block + 16 * g);
+    };
+    auto work = [&](auto at, int kb, int after, float k_scale, float v_scale) {
+        constexpr int x = decltype(at)::value;
+        const bool masked = (kb + 1) * kKv8Block > all_see;  // (the same for the whole block)
+        const int room = t.limit - (kb * kKv8Block + 16 * g);              // of this lane's keys 4 c + e those up to there are seen
         if (masked) {
             // A position that some row does not see may hold anything.  What is no number there must not reach the product, where a
             // weight of 0 would not keep it out; rows that see it get theirs from the flags.
@@ -217,19 +194,19 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) any |= nan_codes(vr[dt][e]);
+                for (int e = 0; e < 4; ++e) any |= nan_codes(vr[x][dt][e]);
             if (__ballot(any != 0)) {
                 f16x8 see[2];
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) see[c >> 1][4 * (c & 1) + e] = (_Float16)(kb * 64 + 16 * g + 4 * c + e > t.limit ? 0.f : 1.f);
+                    for (int e = 0; e < 4; ++e) see[c >> 1][4 * (c & 1) + e] = (_Float16)(4 * c + e > room ? 0.f : 1.f);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) {
                     f32x4 hit{0.f, 0.f, 0.f, 0.f};
                     uint32_t n[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) { n[e] = nan_codes(vr[dt][e]); vr[dt][e] = without_nan(vr[dt][e], n[e]); }
+                    for (int e = 0; e < 4; ++e) { n[e] = nan_codes(vr[x][dt][e]); vr[x][dt][e] = without_nan(vr[x][dt][e], n[e]); }
                     hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(nan_flags(n[0], n[1]), see[0], hit, 0, 0, 0);
                     hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(nan_flags(n[2], n[3]), see[1], hit, 0, 0, 0);
 #pragma unroll
@@ -238,11 +215,92 @@ __global__ __launch_bounds__(256) void attn8_direct_kernel(Kv8AttnArgs a, float 
                 }
             }
         }
+        f32x4 s[4];
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            t.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(vr[dt][0], vr[dt][1]), p[0], t.o[dt], 0, 0, 0);
-            t.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(vr[dt][2], vr[dt][3]), p[1], t.o[dt], 0, 0, 0);
+        for (int c = 0; c < 4; ++c) s[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < KS; ++e)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                s[c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(kr[x][c][e >> 1][2 * (e & 1)], kr[x][c][e >> 1][2 * (e & 1) + 1]), t.q[e], s[c], 0, 0, 0);
+        if (SETS == 1) load_k(at, after);
+        float f = t.unit * k_scale;
+        if (masked) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[c][e] = 4 * c + e > room ? -INFINITY : s[c][e] * f;
+            f = 1.f;
         }
+        float top = s[0][0];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, s[c][e]);
+        top *= f;
+        if (__ballot(top > t.m + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float m = top > t.m + kSlack ? top : t.m, shrink = __builtin_amdgcn_exp2f(t.m - m);
+            t.m = m;
+            t.l *= shrink;
+            large = __ballot(is_large(m)) != 0;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) t.o[dt] *= shrink;
+        }
+        float from = t.m;
+        if (large) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[c][e] = above(s[c][e], f, t.m);
+            f = 1.f;
+            from = 0.f;
+        }
+        // V's scale rides in the weights while it stays within kSlackV of the outputs' unit, which else moves to it
+        float by = v_scale * rvref;
+        if (!(by <= kSlackV && by >= 1.f / kSlackV)) {
+            const float to = vref / v_scale;
+            vref = v_scale;
+            rvref = 1.f / v_scale;
+            by = 1.f;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) t.o[dt] *= to;
+        }
+        const float under = kLift - from + __builtin_amdgcn_logf(by);
+        float sum = 0.f;
+        f16x8 p[2];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                const f16x2 w = __builtin_convertvector((f32x2{__builtin_amdgcn_exp2f(fmaf(s[c][e], f, under)), __builtin_amdgcn_exp2f(fmaf(s[c][e + 1], f, under))}), f16x2);
+                sum = __builtin_amdgcn_fdot2(w, f16x2{1, 1}, sum, false);
+                p[c >> 1][4 * (c & 1) + e] = w[0];
+                p[c >> 1][4 * (c & 1) + e + 1] = w[1];
+            }
+        t.l += sum * __builtin_amdgcn_rcpf(by);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+                t.o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8(vr[x][dt][2 * u], vr[x][dt][2 * u + 1]), p[u], t.o[dt], 0, 0, 0);
+        if (SETS == 1) load_v(at, after);
+    };
+    int kb = first + wave;
+    auto turn = [&](auto now, auto then) {                   // one block; false: it was the last
+        const int after = min(kb + 4, last - 1);
+        float k_scale, v_scale;
+        scales.at(kb, lane, &k_scale, &v_scale);             // (ahead of the loads: a wait for scales would be one for them)
+        if constexpr (SETS == 2) { load_k(then, after); load_v(then, after); }
+        work(now, kb, after, k_scale, v_scale);
+        kb += 4;
+        return kb < last;
+    };
+    if (kb < last) {
+        load_k(Int<0>{}, kb);
+        load_v(Int<0>{}, kb);
+        while (turn(Int<0>{}, Int<SETS - 1>{}) && turn(Int<SETS - 1>{}, Int<0>{})) {}
     }
 
     // join the wavefronts, in their order
@@ -368,6 +426,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     float m = kFarBelow, l = 0.f, vref = 1.f, rvref = 1.f;
+    bool large = false;
     if (first < last) store(0, first >= whole);
     __syncthreads();
 
@@ -408,8 +467,18 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
             const float up = top > m + kSlack ? top : m, shrink = __builtin_amdgcn_exp2f(m - up);
             m = up;
             l *= shrink;
+            large = __ballot(is_large(m)) != 0;
 #pragma unroll
             for (int dt = 0; dt < JT; ++dt) o[dt] *= shrink;
+        }
+        float from = m;
+        if (large) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] = above(s[t][r], f, m);
+            f = 1.f;
+            from = 0.f;
         }
         // V's scale rides in the weights while it stays within kSlackV of the outputs' unit, which else moves to it
         float by = v_scale * rvref;
@@ -421,7 +490,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
 #pragma unroll
             for (int dt = 0; dt < JT; ++dt) o[dt] *= to;
         }
-        const float under = kLift - m + __builtin_amdgcn_logf(by);
+        const float under = kLift - from + __builtin_amdgcn_logf(by);
         float sum = 0.f;
         f16x8 p[4];                                          // p[2 t + u]: keys 32 t + 16 h + 8 u .. + 7
 #pragma unroll
@@ -528,11 +597,31 @@ __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
 // Query rows of a KV head from which on they go 128 to a block
 inline bool use_wide(int NQ) { return NQ > 16; }
 
+// Splits of the keys, so that few rows fill the chip.  Direct kernel: none up to 16 blocks of keys, four for each wavefront (one launch
+// instead of two); then one for four blocks up to eight splits, and up to sixteen on longer caches, while there is a CU for each
+// block of the grid; where the heads alone take more than half of the CUs, as many as are resident, but only on long caches.  us with
+// the join, by splits: 8 heads, 16 blocks 1: 9.5, 4: 9.2; 32 blocks 4: 10.9, 8: 10.6; 63 blocks 4: 12.7, 8: 11.5, 16: 13.2; 501 blocks 8: 31.6,
+// 16: 24.1, 32: 25.9; 64 heads, 63 blocks 4: 17.5, 8: 19.8; 251 blocks 4: 45.6, 8: 47.6; 160 heads, 32 blocks 1: 17.2, 3: 20.1; 126 blocks 1: 68, 3: 58;
+// 256 heads, 63 blocks 1: 41.6, 2: 45.7.
+// Wide kernel: as many as there are CUs for, and twice that where each still walks 16 blocks, three blocks at least to a split.  us: 64 heads
+// (16 x 16 rows x 7 query heads), 65 blocks 2: 51.2, 4: 35.5, 8: 37.4; 48 heads (24 x 5 x 8), 47 blocks 2: 27, 5: 17.1, 10: 18.5; 8 heads (9 rows x 4), 16 blocks 1: 25.5,
+// 5: 13.7, 16: 15.5; 251 blocks 16: 32.8, 32: 28.4; 128 (4 x 33 rows x 32 heads), 17 blocks 1: 27.7, 2: 21.4, 4: 22.3; 64 blocks 2: 49.3, 4: 43.6.
 int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
-    const int NQ = h_q / h_kv * R, rows = use_wide(NQ) ? 128 : 16, chunks = (NQ + rows - 1) / rows, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
-    long splits = 512 / ((long)B * h_kv * chunks);
-    const int most = (blocks + 3) / 4;
-    splits = splits > most ? most : splits;
+    const int NQ = h_q / h_kv * R, rows = use_wide(NQ) ? 128 : 16, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
+    const long heads = (long)B * h_kv * ((NQ + rows - 1) / rows);
+    long splits;
+    if (use_wide(NQ)) {
+        // rows see half of the step's own keys on average
+        const int seen = (len_bound - R / 2 + kKv8Block - 1) / kKv8Block, most = seen / 3;
+        splits = 256 / heads;
+        if (splits > 0 && seen / splits >= 16) splits = 512 / heads;
+        splits = splits > most ? most : splits;
+    } else {
+        if (blocks <= 16) return 1;
+        splits = heads > 128 && heads < 256 && blocks >= 96 ? 512 / heads : 256 / heads;
+        const int by_four = (blocks + 3) / 4, by_ten = blocks / 10 < 16 ? blocks / 10 : 16, most = by_four < 8 ? by_four : by_ten < 8 ? 8 : by_ten;
+        splits = splits > most ? most : splits;
+    }
     return splits < 1 ? 1 : (int)splits;
 }
 

@@ -325,6 +325,24 @@ def test_attention_scores_far_apart_and_scales_far_apart():
         assert np.all(np.abs(got.double().cpu().numpy() - ref) <= _room(ref, weighted))
 
 
+@pytest.mark.parametrize("heads,R", [(1, 3), (2, 40), (5, 60)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_large_scores(heads, R, d):
+    """Scores of 2^20 and 2^100, all equal or far apart: weights of 1 and 0."""
+    n = 64 * 5
+    c = Cache(1, 1, d, n, [0])
+    c.k[0][0].append(0, np.ones((n, d)))
+    c.v[0][0].append(0, np.random.default_rng(R).normal(size=(n, d)))
+    c.k[0][0].append(70, np.full((1, d), 2.0))
+    c.layer = runtime.KV8Layer(*c.tensors(), c.lens)
+    c.lens.fill_(n - R)
+    for size in (2.0 ** 18, 2.0 ** 100, -(2.0 ** 100)):
+        q = (torch.ones(1, R, heads, d) * size * (1 + torch.arange(R).view(1, R, 1, 1) / 128)).to(BF16)
+        got = runtime.KV8Attention()(c.layer, q.cuda(), len_upper_bound=n)
+        ref, weighted = _attention_oracle(c, q.double().numpy(), [n - R], R, 1 / math.sqrt(d))
+        assert np.all(np.abs(got.double().cpu().numpy() - ref) <= _room(ref, weighted)), size
+
+
 def test_attention_over_more_than_four_gigabytes_of_codes():
     """Zero codes but for two far tokens of the last head: byte offsets beyond 2^32."""
     h, d, n = 9, 128, 1 << 22
