@@ -266,7 +266,9 @@ struct Kv8AppendArgs {
     void *q_out;                  // rotated queries, rows q_out_stride elements apart; NULL: no queries
     int64_t q_out_stride;
     int B, R, h_q, h_kv, d_h, max_len;
-    int units;                    // these two: set by launch_kv8_append
+    int units;                    // these: set by launch_kv8_append
+    int q_rows, q_parts;          // rows of a block of queries, blocks of a group of rows
+    FastDiv per_row, by_r;        // items of a row's queries; R
     bool q_vec;
     RopeParams rope;              // rot 0: nothing turns
     const float2 *cs;             // the rows' (cos, sin), rows cs_stride pairs apart; NULL: worked out from `turns`

@@ -150,7 +150,7 @@ __device__ __forceinline__ uint32_t shrink4(uint32_t w, float ratio) {
 
 // One launch, blocks of two kinds.  The first `units` blocks: the new tokens of one cache block of one KV head, K or V.  Thread t has the
 // items t and t + 256 of 64 rows x d / 16: their entries stay in registers from the one read, through the block's maximum, to
-// the codes.  The others rotate query heads, 512 items each.
+// the codes.  The others rotate the query heads of up to 16 rows, 512 items, by angles that the block works out once for all heads.
 // What bounds it: bytes for prompts, the chain load -> maximum -> scale -> store for few rows.
 template <typename Rows, typename TQ, bool ODD>
 __global__ __launch_bounds__(kThreads) void kv8_append_kernel(Kv8AppendArgs a, Rows xq, Rows xk, Rows xv) {
@@ -176,52 +176,58 @@ __global__ __launch_bounds__(kThreads) void kv8_append_kernel(Kv8AppendArgs a, R
     };
 
     if ((int)blockIdx.x >= a.units) {
-        const int64_t items = (int64_t)a.B * R * a.h_q * per_head;
-        const int64_t i0 = (int64_t)(blockIdx.x - a.units) * (kThreads * kQueryItems);
+        const int part = (blockIdx.x - a.units) % a.q_parts, m0 = (blockIdx.x - a.units) / a.q_parts * a.q_rows;
+        const int rows = min(a.q_rows, a.B * R - m0), left = rows * (int)a.per_row.n - part * (kThreads * kQueryItems);
+        float2 *cs = reinterpret_cast<float2 *>(s_codes);    // [rows][rot / 2], worked out once for all heads
+        auto place = [&](int m) { return min(max(a.lens[a.by_r.div(m)], 0), a.max_len) + m - (int)a.by_r.div(m) * R; };
         float u[kQueryItems][8], v[kQueryItems][8];
         Item it[kQueryItems];
-        int64_t m[kQueryItems];
-        int head[kQueryItems], pos[kQueryItems];
-        const int64_t m0 = i0 / (a.h_q * per_head);
-        const int left = (int)min((int64_t)(kThreads * kQueryItems), items - i0);
+        int row[kQueryItems], head[kQueryItems], j[kQueryItems];
 #pragma unroll
         for (int k = 0; k < kQueryItems; ++k) {
-            const int i = min(k * kThreads + tid, left - 1) + (int)(i0 - m0 * (a.h_q * per_head));
-            m[k] = m0 + i / (a.h_q * per_head);
-            const int in_row = i % (a.h_q * per_head);
+            const int i = min(k * kThreads + tid, left - 1) + part * (kThreads * kQueryItems);
+            row[k] = a.per_row.div(i);
+            const int in_row = i - row[k] * (int)a.per_row.n;
             head[k] = in_row / per_head;
-            pos[k] = min(max(a.lens[m[k] / R], 0), a.max_len) + (int)(m[k] % R);
-            it[k] = load_item<ODD>(xq, m[k], (int64_t)head[k] * d, in_row % per_head, rot, interleaved, u[k], v[k],
-                                   [&](int f) { return cs_of(m[k], pos[k], f); });
+            j[k] = in_row % per_head;
+            if constexpr (!ODD) it[k] = load_item<ODD>(xq, m0 + row[k], (int64_t)head[k] * d, j[k], rot, interleaved, u[k], v[k], [](int) { return float2{}; });
         }
-        if (a.rs.sumsq) {
-            const int64_t mn = (i0 + left - 1) / (a.h_q * per_head) - m0 + 1;
-            row_scale(m0, (int)min(mn, (int64_t)kKv8Block));
+        for (int f = tid; f < rows * (rot / 2); f += kThreads) {
+            const int r = f / (rot / 2);
+            cs[f] = cs_of(m0 + r, a.cs ? 0 : place(m0 + r), f - r * (rot / 2));
         }
+        __syncthreads();
+        if constexpr (ODD) {
+#pragma unroll
+            for (int k = 0; k < kQueryItems; ++k)
+                it[k] = load_item<ODD>(xq, m0 + row[k], (int64_t)head[k] * d, j[k], rot, interleaved, u[k], v[k], [&](int f) { return cs[row[k] * (rot / 2) + f]; });
+            __syncthreads();                                 // partners are read across threads: in place, before any is written
+        }
+        if (a.rs.sumsq) row_scale(m0, rows);
 #pragma unroll
         for (int k = 0; k < kQueryItems; ++k) {
             if (k * kThreads + tid >= left) continue;
-            turn_item(it[k], interleaved, u[k], v[k], [&](int f) { return cs_of(m[k], pos[k], f); });
-            const float sc = a.rs.sumsq ? s_row[m[k] - m0] : 1.0f;
-            TQ *dst = (TQ *)a.q_out + m[k] * a.q_out_stride + (int64_t)head[k] * d;
+            turn_item(it[k], interleaved, u[k], v[k], [&](int f) { return cs[row[k] * (rot / 2) + f]; });
+            const float sc = a.rs.sumsq ? s_row[row[k]] : 1.0f;
+            TQ *dst = (TQ *)a.q_out + (m0 + row[k]) * a.q_out_stride + (int64_t)head[k] * d;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) { u[k][j] *= sc; v[k][j] *= sc; }
+            for (int e = 0; e < 8; ++e) { u[k][e] *= sc; v[k][e] *= sc; }
             if (a.q_vec) {
                 if constexpr (sizeof(TQ) == 2) {
                     *reinterpret_cast<u32x4 *>(dst + it[k].e0) = u32x4{pack_bf16x2(u[k][0], u[k][1]), pack_bf16x2(u[k][2], u[k][3]), pack_bf16x2(u[k][4], u[k][5]), pack_bf16x2(u[k][6], u[k][7])};
                     *reinterpret_cast<u32x4 *>(dst + it[k].e1) = u32x4{pack_bf16x2(v[k][0], v[k][1]), pack_bf16x2(v[k][2], v[k][3]), pack_bf16x2(v[k][4], v[k][5]), pack_bf16x2(v[k][6], v[k][7])};
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; j += 4) {
-                        *reinterpret_cast<f32x4 *>(dst + it[k].e0 + j) = f32x4{u[k][j], u[k][j + 1], u[k][j + 2], u[k][j + 3]};
-                        *reinterpret_cast<f32x4 *>(dst + it[k].e1 + j) = f32x4{v[k][j], v[k][j + 1], v[k][j + 2], v[k][j + 3]};
+                    for (int e = 0; e < 8; e += 4) {
+                        *reinterpret_cast<f32x4 *>(dst + it[k].e0 + e) = f32x4{u[k][e], u[k][e + 1], u[k][e + 2], u[k][e + 3]};
+                        *reinterpret_cast<f32x4 *>(dst + it[k].e1 + e) = f32x4{v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3]};
                     }
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    store_elem(dst, it[k].e0 + j, u[k][j]);
-                    store_elem(dst, it[k].e1 + j, v[k][j]);
+                for (int e = 0; e < 8; ++e) {
+                    store_elem(dst, it[k].e0 + e, u[k][e]);
+                    store_elem(dst, it[k].e1 + e, v[k][e]);
                 }
             }
         }
@@ -344,8 +350,12 @@ void launch_kv8_append(const Kv8AppendArgs &args, const Kv8Source &src, hipStrea
     Kv8AppendArgs a = args;
     const int blocks = (a.R + kKv8Block - 2) / kKv8Block + 1;                              // at most, of one sequence
     a.units = 2 * a.B * a.h_kv * blocks;
-    const int64_t items = a.q_out ? (int64_t)a.B * a.R * a.h_q * (a.d_h / 16) : 0;
-    const unsigned grid = (unsigned)(a.units + (items + kThreads * kQueryItems - 1) / (kThreads * kQueryItems));
+    const int per_row = a.h_q * (a.d_h / 16), per_block = kThreads * kQueryItems;
+    a.q_rows = per_row >= per_block ? 1 : per_block / per_row < 16 ? per_block / per_row : 16;           // (16 rows of 64 angles fill the LDS)
+    a.q_parts = (a.q_rows * per_row + per_block - 1) / per_block;
+    a.per_row = FastDiv(per_row);
+    a.by_r = FastDiv(a.R);
+    const unsigned grid = a.units + (a.q_out ? (a.B * a.R + a.q_rows - 1) / a.q_rows * a.q_parts : 0);
     const bool odd = a.rope.rot % 16 != 0;
     const int out_es = src.bf16 ? 2 : 4;
     a.q_vec = (uintptr_t)a.q_out % 16 == 0 && a.q_out_stride * out_es % 16 == 0;

@@ -193,6 +193,9 @@ def test_append(case):
     state = [t.clone() for t in c.state()]
     c.layer.append(q, k, v, r, len_upper_bound=max(lens) + R, q_out=torch.empty_like(q_out))
     assert _same_bits(state, c.state())
+    # in place, in the buffer of projections
+    again = c.layer.append(q, k, v, r, len_upper_bound=max(lens) + R, q_out=q)
+    assert again.data_ptr() == q.data_ptr() and torch.equal(q, q_out) and _same_bits(state, c.state())
     r.close()
 
 
