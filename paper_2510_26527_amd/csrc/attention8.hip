@@ -331,74 +331,91 @@ __global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, flo
     }
 }
 
-// Many query rows: four wavefronts of 32 rows each, on the 32 x 32 matrix instructions, walk the same keys.  The codes of 64 keys, 16 KB at
-// d_head 128, pass through LDS once for the block, in the order of the operands: a piece of 1 KB is what the 64 lanes read at
-// once, sixteen codes each, and becomes two operands.  Row x of K's tile t is key 32 t + 16 (x / 4 % 2) + 4 (x / 8) + x % 4, so that
-// a lane's scores, of keys 32 t + 16 h .. + 15 for lane half h, are in the order of V's pieces.
-template <int DH, bool QB, int OUT>
-__global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float scale_log2) {
-    constexpr int JT = DH / 32, PIECES = 4 * JT, MINE = PIECES / 4;        // K: 2 JT pieces [t][j], V: 2 JT [dt][w]
-    __shared__ u32x4 s_tile[2][PIECES][64];
-    __shared__ int s_nan[2][2];
+// The wide kernel's LDS: two sets of codes; afterwards what the groups hand to the first one; then rows on their way out, 16 bytes apart
+template <int DH, int QG, int KG, int OUT>
+constexpr int wide_lds() {
+    constexpr int JT = DH / 32, stage = 2 * KG * 4 * JT * 1024, join = KG > 1 ? (KG - 1) * QG * (JT * 4096 + 512) : 0;
+    constexpr int rows = QG * 32 * (DH * (OUT == kOutF32 || OUT == kOutPart ? 4 : 2) + 16);
+    return stage > join ? (stage > rows ? stage : rows) : (join > rows ? join : rows);
+}
+
+// Many query rows: wavefronts of 32 rows each on the 32 x 32 matrix instructions, QG of them side by side on the rows of a block and KG such
+// groups on different blocks of keys, joined in LDS at the end.  The codes of 64 keys, 16 KB at d_head 128, pass through LDS once for
+// a group, in the order of the operands: a piece of 1 KB is what the 64 lanes read at once, sixteen codes each, and becomes two
+// operands.  Row x of K's tile t is key 32 t + 16 (x / 4 % 2) + 4 (x / 8) + x % 4, so that a lane's scores, of keys 32 t + 16 h .. + 15 for lane
+// half h, are in the order of V's pieces.
+// What bounds it: a wavefront's own chain of LDS reads, scores, maximum, weights and product (xx clocks a block of keys, of which 1024 are
+// matrix instructions), which two wavefronts a SIMD overlap.  Eight wavefronts, KG = 2, rather than two blocks of four a CU: the blocks of
+// a prompt's last rows, which walk most keys, are then walked at that rate to their end.
+template <int DH, int QG, int KG, bool QB, int OUT>
+__global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide_kernel(Kv8AttnArgs a, float scale_log2, FastDiv by_group) {
+    constexpr int JT = DH / 32, PIECES = 4 * JT, MINE = PIECES / QG;       // K: 2 JT pieces [t][j], V: 2 JT [dt][w]
+    constexpr int kRowBytes = DH * (OUT == kOutF32 || OUT == kOutPart ? 4 : 2) + 16;
+    static_assert(wide_lds<DH, QG, KG, OUT>() <= 159 * 1024, "LDS");
+    extern __shared__ __attribute__((aligned(16))) uint8_t s_raw[];
+    __shared__ int s_nan[2][KG][QG];
+    auto tile = [&](int set, int group) { return reinterpret_cast<u32x4 (*)[64]>(s_raw + (set * KG + group) * PIECES * 1024); };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 31, h = lane >> 5;
+    const int qg = wave % QG, kg = wave / QG;
     // Blocks by how many keys they walk, most first, a head's chunk before the next chunk; those that fill the chip's second places
     // the other way round, so that where all are resident at once a long one shares its CU with a short one.
     uint32_t rank = blockIdx.x + gridDim.x * blockIdx.z;
     if (rank >= 256u && gridDim.x * gridDim.z <= 512u) rank = 255u + gridDim.x * gridDim.z - rank;
-    const int bh = rank % gridDim.x, b = bh / a.h_kv, hk = bh % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
+    const int bh = rank % gridDim.x, b = bh / a.h_kv, hk = bh % a.h_kv, group = by_group.n, NQ = group * a.R;
     const int split = blockIdx.y, chunk = gridDim.z - 1 - rank / gridDim.x;
     const int len = min(max(a.lens[b], 0), a.max_len);
     const int n_keys = min(len + a.R, a.max_len);
-    const int q0 = chunk * 128 + wave * 32, qi = q0 + i;
-    const int row = min(qi, NQ - 1) / group, head = hk * group + min(qi, NQ - 1) % group;
+    const int c0 = chunk * (QG * 32), q0 = c0 + qg * 32, qi = q0 + i;
+    const int row = by_group.div(min(qi, NQ - 1)), head = hk * group + min(qi, NQ - 1) - row * group;
     const int limit = qi < NQ ? len + row : -1;
     // keys that some row of the block, some row of the wavefront sees
-    const int block_seen = min(len + min(chunk * 128 + 127, NQ - 1) / group + 1, n_keys);
-    const int wave_seen = q0 < NQ ? min(len + min(q0 + 31, NQ - 1) / group + 1, n_keys) : 0;
+    const int block_seen = min(len + (int)by_group.div(min(c0 + QG * 32, NQ) - 1) + 1, n_keys);
+    const int wave_seen = q0 < NQ ? min(len + (int)by_group.div(min(q0 + 32, NQ) - 1) + 1, n_keys) : 0;
     const int n_blocks = (block_seen + kKv8Block - 1) / kKv8Block;
     const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
-    const int whole = min(last, (len + chunk * 128 / group + 1) / kKv8Block);              // blocks of keys below that every row of the block sees
+    const int whole = min(last, (len + (int)by_group.div(c0) + 1) / kKv8Block);            // blocks of keys below that every row of the block sees
     const size_t cache_row = (size_t)b * a.h_kv + hk;
     const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
     const size_t scale_row = cache_row * (a.max_len / kKv8Block);
     Scales scales{a.k_scale + scale_row, a.v_scale + scale_row, n_blocks, 0, 0.f, 0.f};
 
-    // a wavefront brings pieces of one kind: this lane's part of them lies these bytes into a block
-    const uint8_t *mine = wave < 2 ? K : V;
+    // every wavefront brings some of K's and as many of V's pieces of its group's block
     uint32_t src[MINE];
 #pragma unroll
     for (int c = 0; c < MINE; ++c) {
-        const int x = (wave & 1) * MINE + c;
-        src[c] = wave < 2 ? (32 * (x / JT) + 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3)) * DH + 32 * (x % JT) + 16 * h
-                          : (32 * (x / 2) + i) * kKv8Block + 32 * (x % 2) + 16 * h;
+        const int x = (c * QG + qg) % (2 * JT);
+        src[c] = c < MINE / 2 ? (32 * (x / JT) + 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3)) * DH + 32 * (x % JT) + 16 * h
+                              : (32 * (x / 2) + i) * kKv8Block + 32 * (x % 2) + 16 * h;
     }
     u32x4 next[MINE];
-    auto load = [&](int kb) {
-        const uint8_t *block = mine + (size_t)kb * kKv8Block * DH;
+    auto load = [&](int kt) {
+        const size_t at = (size_t)min(kt, last - 1) * kKv8Block * DH;
 #pragma unroll
-        for (int c = 0; c < MINE; ++c) next[c] = *reinterpret_cast<const u32x4 *>(block + src[c]);
+        for (int c = 0; c < MINE; ++c) next[c] = *reinterpret_cast<const u32x4 *>((c < MINE / 2 ? K : V) + at + src[c]);
     };
     // look: a block that needs the mask.  A position that some row does not see may hold anything: what is no number among V's entries
     // must not reach the product, where a weight of 0 would not keep it out.
     auto store = [&](int set, bool look) {
-        if (look && wave >= 2) {
+        if (look) {
             uint32_t any = 0;
 #pragma unroll
-            for (int c = 0; c < MINE; ++c)
+            for (int c = MINE / 2; c < MINE; ++c)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint32_t n = nan_codes(next[c][e]);
-                    any |= n;
-                    next[c][e] = without_nan(next[c][e], n);
-                }
+                for (int e = 0; e < 4; ++e) any |= nan_codes(next[c][e]);
             const bool found = __ballot(any != 0) != 0;
-            if (lane == 0) s_nan[set][wave - 2] = found;
+            if (found) {
+#pragma unroll
+                for (int c = MINE / 2; c < MINE; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) next[c][e] = without_nan(next[c][e], nan_codes(next[c][e]));
+            }
+            if (lane == 0) s_nan[set][kg][qg] = found;
         }
 #pragma unroll
-        for (int c = 0; c < MINE; ++c) s_tile[set][wave * MINE + c][lane] = next[c];
+        for (int c = 0; c < MINE; ++c) tile(set, kg)[c * QG + qg][lane] = next[c];
     };
     if (first < last) {
-        load(first);
+        load(first + kg);
         scales.fetch(first, lane);
     }
 
@@ -427,13 +444,13 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
         for (int r = 0; r < 16; ++r) o[dt][r] = 0.f;
     float m = kFarBelow, l = 0.f, vref = 1.f, rvref = 1.f;
     bool large = false;
-    if (first < last) store(0, first >= whole);
+    if (first < last) store(0, first + KG > whole);
     __syncthreads();
 
     auto step = [&](auto with_mask, int kb, int set, float k_scale, float v_scale) {
         constexpr bool MASKED = decltype(with_mask)::value != 0;
         const int room = limit - (kb * kKv8Block + 16 * h);  // of this lane's keys 32 t + r those up to there are seen
-        const u32x4 (*tile)[64] = s_tile[set];
+        const u32x4 (*codes)[64] = tile(set, kg);
         f32x16 s[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -445,7 +462,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const u32x4 w = tile[t * JT + j][lane];
+                    const u32x4 w = codes[t * JT + j][lane];
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2 * u], w[2 * u + 1]), q[2 * j + u], s[t], 0, 0, 0);
                 }
         float f = unit * k_scale;
@@ -509,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int dt = 0; dt < JT; ++dt) {
-                    const u32x4 w = tile[2 * JT + 2 * dt + x][lane];
+                    const u32x4 w = codes[2 * JT + 2 * dt + x][lane];
                     o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(widen8(w[2 * u], w[2 * u + 1]), p[2 * x + u], o[dt], 0, 0, 0);
                 }
     };
@@ -537,39 +554,119 @@ __global__ __launch_bounds__(256, 2) void attn8_wide_kernel(Kv8AttnArgs a, float
                 if (hit[r] > 0.f) o[dt][r] = __uint_as_float(0x7fc00000u);
         }
     };
-    // blocks of keys that every row of the block sees, then those that need the mask
+    // blocks of keys that every row of the block sees, then those that need the mask: KG at a time, one for each group
     int kb = first, set = 0;
     auto walk = [&](auto with_mask, int end) {
-        for (; kb < end; ++kb, set ^= 1) {
+        for (; kb < end; kb += KG, set ^= 1) {
+            const int kt = kb + kg;
             float k_scale, v_scale;
-            scales.at(kb, lane, &k_scale, &v_scale);         // (ahead of the loads: a wait for scales would be one for them)
-            load(kb + 1 < last ? kb + 1 : kb);
+            scales.at(min(kt, last - 1), lane, &k_scale, &v_scale);        // (ahead of the loads: a wait for scales would be one for them)
+            load(kt + KG);
             if constexpr (decltype(with_mask)::value == 0) {
-                step(with_mask, kb, set, k_scale, v_scale);
-            } else if (kb * kKv8Block < wave_seen) {         // (the same for the wavefront)
-                if (s_nan[set][0] | s_nan[set][1]) holes(kb);
-                step(with_mask, kb, set, k_scale, v_scale);
+                step(with_mask, kt, set, k_scale, v_scale);
+            } else if (kt < last && kt * kKv8Block < wave_seen) {          // (the same for the wavefront)
+                int bad = 0;
+#pragma unroll
+                for (int x = 0; x < QG; ++x) bad |= s_nan[set][kg][x];
+                if (__builtin_amdgcn_readfirstlane(bad)) holes(kt);
+                step(with_mask, kt, set, k_scale, v_scale);
             }
-            store(set ^ 1, kb + 1 >= whole);                                  // nobody reads that set any more: all are past the last barrier
+            store(set ^ 1, kb + 2 * KG > whole);             // (look: as for `plain`)  nobody reads that set any more: all are past the last barrier
             __syncthreads();
         }
     };
-    walk(Int<0>{}, whole);
+    const int plain = first + (whole > first ? (whole - first) / KG * KG : 0);
+    walk(Int<0>{}, plain);
     walk(Int<1>{}, last);
 
+    if constexpr (KG > 1) {                                  // the groups' results, in their order
+        f32x4 (*s_o)[JT * 4][64] = reinterpret_cast<f32x4 (*)[JT * 4][64]>(s_raw);
+        float2 (*s_ml)[64] = reinterpret_cast<float2 (*)[64]>(s_raw + (KG - 1) * QG * JT * 4096);
+        if (kg) {
+            const int at = (kg - 1) * QG + qg;
+            s_ml[at][lane] = make_float2(m, l);
+#pragma unroll
+            for (int dt = 0; dt < JT; ++dt)
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    s_o[at][dt * 4 + x][lane] = f32x4{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]} * vref;
+        }
+        __syncthreads();
+        if (kg == 0) {
+            float M = m;
+#pragma unroll
+            for (int g = 1; g < KG; ++g) M = fmaxf(M, s_ml[(g - 1) * QG + qg][lane].x);
+            const float mine = __builtin_amdgcn_exp2f(m - M);
+            l *= mine;
+#pragma unroll
+            for (int dt = 0; dt < JT; ++dt) o[dt] *= vref * mine;
+            vref = 1.f;
+            m = M;
+#pragma unroll
+            for (int g = 1; g < KG; ++g) {
+                const int at = (g - 1) * QG + qg;
+                const float2 ml = s_ml[at][lane];
+                const float w = __builtin_amdgcn_exp2f(ml.x - M);
+                l += ml.y * w;
+#pragma unroll
+                for (int dt = 0; dt < JT; ++dt)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const f32x4 r = s_o[at][dt * 4 + x][lane];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[dt][4 * x + e] += r[e] * w;
+                    }
+            }
+        }
+        __syncthreads();
+        if (kg) return;
+    }
     l += __shfl_xor(l, 32, kWave);
-    if (qi >= NQ) return;
-    const int64_t mrow = (int64_t)b * a.R + row;
     const float inv = l != 0.f ? vref / l : 0.f;             // (a split none of whose keys the row sees: 0; a sum that is no number is not 0)
+    const int64_t mrow = (int64_t)b * a.R + row;
+    if (OUT == kOutPart && h == 0 && qi < NQ) a.part_ml[(mrow * a.h_q + head) * a.splits + split] = make_float2(m, l);
+    if constexpr (OUT == kOutOp) {
+        if (qi >= NQ) return;
 #pragma unroll
-    for (int dt = 0; dt < JT; ++dt)
+        for (int dt = 0; dt < JT; ++dt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-            store_out4<OUT>(a, mrow, head, split, 32 * dt + 8 * x + 4 * h,
-                            f32x4{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]} * inv);
-    if (OUT == kOutPart && h == 0) a.part_ml[(mrow * a.h_q + head) * a.splits + split] = make_float2(m, l);
+            for (int x = 0; x < 4; ++x)
+                op_store4(a.out_op, (int)mrow, head * DH + 32 * dt + 8 * x + 4 * h, a.op_folded,
+                          f32x4{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]} * inv);
+    } else {
+        // rows through LDS, the wavefront's own part of it, so that they leave sixteen bytes a lane side by side: eight bytes a lane into
+        // 32 rows took 2 us at the end of every block
+        constexpr bool HALF = OUT == kOutBf16 || OUT == kOutF16;
+        constexpr int PER = DH * (HALF ? 2 : 4) / 16;        // lanes of a row
+        uint8_t *rows = s_raw + qg * 32 * kRowBytes;
+#pragma unroll
+        for (int dt = 0; dt < JT; ++dt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const f32x4 r = f32x4{o[dt][4 * x], o[dt][4 * x + 1], o[dt][4 * x + 2], o[dt][4 * x + 3]} * inv;
+                uint8_t *at = rows + i * kRowBytes + (32 * dt + 8 * x + 4 * h) * (HALF ? 2 : 4);
+                if constexpr (OUT == kOutBf16) *reinterpret_cast<uint2 *>(at) = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
+                else if constexpr (OUT == kOutF16)
+                    *reinterpret_cast<uint2 *>(at) = make_uint2(f32_to_f16_bits(r[0]) | ((uint32_t)f32_to_f16_bits(r[1]) << 16), f32_to_f16_bits(r[2]) | ((uint32_t)f32_to_f16_bits(r[3]) << 16));
+                else *reinterpret_cast<f32x4 *>(at) = r;
+            }
+        __builtin_amdgcn_wave_barrier();                     // (a wavefront's LDS accesses are in order)
+#pragma unroll
+        for (int x = 0; x < 32 * PER / 64; ++x) {
+            const int r = (x * 64 + lane) / PER, piece = (x * 64 + lane) % PER;
+            const u32x4 w = *reinterpret_cast<const u32x4 *>(rows + r * kRowBytes + piece * 16);
+            if (q0 + r >= NQ) continue;
+            const int rr = by_group.div(q0 + r), hh = hk * group + q0 + r - rr * group;
+            const int64_t mr = (int64_t)b * a.R + rr;
+            uint8_t *dst;
+            if constexpr (OUT == kOutBf16) dst = (uint8_t *)(a.out_bf16 + mr * a.out_stride + hh * DH);
+            else if constexpr (OUT == kOutF16) dst = (uint8_t *)(a.out16 + (mr * a.h_q + hh) * DH);
+            else if constexpr (OUT == kOutF32) dst = (uint8_t *)(a.out + (mr * a.h_q + hh) * DH);
+            else dst = (uint8_t *)(a.part_o + ((mr * a.h_q + hh) * a.splits + split) * DH);
+            *reinterpret_cast<u32x4 *>(dst + piece * 16) = w;
+        }
+    }
 }
-
 // Joins the splits of a row and head, in their order: 64 / (d_h / 4) of them a wavefront, four entries a lane.
 template <int DH, int OUT>
 __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
@@ -594,8 +691,8 @@ __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
 
 }  // namespace
 
-// Query rows of a KV head from which on they go 128 to a block
-inline bool use_wide(int NQ) { return NQ > 16; }
+// Query rows of a KV head that go to a block: up to 16 the direct kernel's, above the wide kernel's
+inline int wide_rows(int NQ) { return NQ > 64 ? 128 : NQ > 16 ? 64 : 16; }
 
 // Splits of the keys, so that few rows fill the chip.  Direct kernel: none up to 16 blocks of keys, four for each wavefront (one launch
 // instead of two); then one for four blocks up to eight splits, and up to sixteen on longer caches, while there is a CU for each
@@ -607,10 +704,10 @@ inline bool use_wide(int NQ) { return NQ > 16; }
 // (16 x 16 rows x 7 query heads), 65 blocks 2: 51.2, 4: 35.5, 8: 37.4; 48 heads (24 x 5 x 8), 47 blocks 2: 27, 5: 17.1, 10: 18.5; 8 heads (9 rows x 4), 16 blocks 1: 25.5,
 // 5: 13.7, 16: 15.5; 251 blocks 16: 32.8, 32: 28.4; 128 (4 x 33 rows x 32 heads), 17 blocks 1: 27.7, 2: 21.4, 4: 22.3; 64 blocks 2: 49.3, 4: 43.6.
 int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
-    const int NQ = h_q / h_kv * R, rows = use_wide(NQ) ? 128 : 16, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
+    const int NQ = h_q / h_kv * R, rows = wide_rows(NQ), blocks = (len_bound + kKv8Block - 1) / kKv8Block;
     const long heads = (long)B * h_kv * ((NQ + rows - 1) / rows);
     long splits;
-    if (use_wide(NQ)) {
+    if (rows > 16) {
         // rows see half of the step's own keys on average
         const int seen = (len_bound - R / 2 + kKv8Block - 1) / kKv8Block, most = seen / 3;
         splits = 256 / heads;
@@ -650,8 +747,15 @@ void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
         auto go = [&](auto dh, auto qb, auto out) {
             constexpr int DH = decltype(dh)::value, OUT = decltype(out)::value;
             constexpr bool QB = decltype(qb)::value != 0;
-            if (use_wide(NQ))
-                launch_kernel(attn8_wide_kernel<DH, QB, OUT>, dim3(a.B * a.h_kv, a.splits, (NQ + 127) / 128), 256, 0, stream, a, scale_log2);
+            auto wide = [&](auto qg, auto kg) {
+                constexpr int QG = decltype(qg)::value, KG = decltype(kg)::value, lds = wide_lds<DH, QG, KG, OUT>();
+                const auto kernel = attn8_wide_kernel<DH, QG, KG, QB, OUT>;
+                if (lds > 64 * 1024)                         // more than a kernel gets unasked
+                    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+                launch_kernel(kernel, dim3(a.B * a.h_kv, a.splits, (NQ + QG * 32 - 1) / (QG * 32)), QG * KG * 64, lds, stream, a, scale_log2, FastDiv(a.h_q / a.h_kv));
+            };
+            if (wide_rows(NQ) == 128) wide(Int<4>{}, Int<1>{});
+            else if (wide_rows(NQ) == 64) wide(Int<2>{}, Int<2>{});
             else
                 launch_kernel(attn8_direct_kernel<DH, QB, OUT>, dim3(a.splits, (NQ + 15) / 16, a.B * a.h_kv), 256, 0, stream, a, scale_log2);
         };
