@@ -130,10 +130,13 @@ def _current(*tensors):
 
 def _row_stride(t):
     """Elements between the rows of t [..., heads, d], whose heads are dense within a row, and rows evenly apart."""
-    shape, strides = t.shape, t.stride()
+    shape = t.shape
     width = shape[-2] * shape[-1]
     if t.is_contiguous():
         return width
+    strides = t.stride()
+    if len(shape) == 4 and strides[3] == 1 and strides[2] == shape[3] and strides[0] == strides[1] * shape[1]:
+        return strides[1]                                    # [B, R, heads, d] of a buffer of projections
     if strides[-1] != 1 or (shape[-2] > 1 and strides[-2] != shape[-1]):
         raise ValueError("a row's heads have to lie side by side")
     stride, span = None, 1
