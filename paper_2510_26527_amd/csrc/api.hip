@@ -299,7 +299,8 @@ namespace {
 
 struct ForwardPlan {
     int M, width_qkv;
-    int sk_qkv, sk_o, sk_gu, sk_down, sk_head, attn_splits, attn_range;
+    int sk_qkv, sk_o, sk_gu, sk_down, sk_head, attn_splits;
+    Kv8AttnPlan kv8;              // on an 8-bit cache
     size_t off_x, off_xn, off_q, off_attn, off_h, off_partial, off_po, off_pml, off_sumsq, off_rope, off_tilectr, off_tree, total;
     size_t off_xn16, off_attn16, off_h16;
     bool half_copies;             // bf16, M > kStreamMaxRows or 4-bit projections: the producers also leave fp16 copies of the activations
@@ -374,11 +375,10 @@ void plan_layout(const psd_model *mdl, int batch, int n_new, int len_bound, bool
     const int M = p.M, hd = d.n_q_heads * d.d_head;
     const int n_o[1] = {d.d_model};
     p.fused_rope = !q8 && !mdl->pairs() && attn_fuses_rope(d.dtype, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, tree);
-    p.attn_range = 0;
-    if (q8)
-        p.attn_splits = any_len ? kv8_attn_max_splits(batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, len_bound)
-                                : kv8_attn_splits(batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, len_bound, &p.attn_range);
-    else
+    if (q8) {
+        p.kv8 = kv8_attn_plan(batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, len_bound);
+        p.attn_splits = any_len ? kv8_attn_max_splits(batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head, len_bound) : p.kv8.splits;
+    } else
         p.attn_splits = (any_len ? attn_max_splits : attn_pick_splits)(d.dtype, batch, n_new, d.n_q_heads, d.n_kv_heads, d.d_head,
                                                                        len_bound, tree);
     const size_t act = 4;                                    // activations are fp32 for both dtypes
@@ -598,7 +598,7 @@ static psd_status forward_once(psd_model *m, const int32_t *tokens_dev, int32_t 
             Kv8AttnArgs at{};
             at.q = q; at.q_stride = hd; at.k = (const uint8_t *)kl; at.v = (const uint8_t *)vl; at.k_scale = ap.k_scale; at.v_scale = ap.v_scale;
             at.lens = kv->lens; at.B = B; at.R = n_new; at.h_q = d.n_q_heads; at.h_kv = d.n_kv_heads; at.d_h = d.d_head; at.max_len = kv->max_len;
-            at.scale = 1.0f / sqrtf((float)d.d_head); at.splits = p.attn_splits; at.range = p.attn_range;
+            at.scale = 1.0f / sqrtf((float)d.d_head); at.plan = p.kv8;
             at.out16 = attn16;
             if (!p.half_copies) { if (p.folded) at.out_op = (uint16_t *)attn; else at.out = attn; }
             at.op_folded = op_folded; at.part_o = (float *)(ws + p.off_po); at.part_ml = (float2 *)(ws + p.off_pml);
@@ -964,7 +964,7 @@ size_t psd_kv8_attention_workspace_bytes(int32_t batch, int32_t n_new, int32_t n
                                          int32_t len_upper_bound) {
     if (batch <= 0 || n_new <= 0 || n_kv_heads <= 0 || n_q_heads <= 0 || n_q_heads % n_kv_heads || len_upper_bound <= 0) return 0;
     size_t ml = 0;
-    return kv8_attention_scratch(batch, n_new, n_q_heads, d_head, kv8_attn_splits(batch, n_new, n_q_heads, n_kv_heads, d_head, len_upper_bound, nullptr), &ml);
+    return kv8_attention_scratch(batch, n_new, n_q_heads, d_head, kv8_attn_plan(batch, n_new, n_q_heads, n_kv_heads, d_head, len_upper_bound).splits, &ml);
 }
 
 psd_status psd_kv8_attention(const psd_kv8_view *cache, const void *q, void *out, int32_t n_new, int32_t n_q_heads, float scale,
@@ -981,10 +981,10 @@ psd_status psd_kv8_attention(const psd_kv8_view *cache, const void *q, void *out
     a.k = (const uint8_t *)cache->k_codes; a.v = (const uint8_t *)cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
     a.lens = cache->lens; a.B = cache->batch; a.R = n_new; a.h_q = n_q_heads; a.h_kv = cache->n_kv_heads; a.d_h = cache->d_head;
     a.max_len = cache->max_len; a.scale = scale == 0.f ? 1.0f / sqrtf((float)cache->d_head) : scale;
-    a.splits = kv8_attn_splits(a.B, a.R, a.h_q, a.h_kv, a.d_h, len_upper_bound, &a.range);
+    a.plan = kv8_attn_plan(a.B, a.R, a.h_q, a.h_kv, a.d_h, len_upper_bound);
     a.out_bf16 = (uint16_t *)out; a.out_stride = out_row_stride;
     size_t ml = 0;
-    const size_t need = kv8_attention_scratch(a.B, a.R, a.h_q, a.d_h, a.splits, &ml);
+    const size_t need = kv8_attention_scratch(a.B, a.R, a.h_q, a.d_h, a.plan.splits, &ml);
     if (need) {
         if (!workspace || (uintptr_t)workspace % 256 || ws_bytes < need) return PSD_ERR_WORKSPACE;
         a.part_o = (float *)workspace;

@@ -83,7 +83,7 @@ __device__ __forceinline__ void store_out4(const Kv8AttnArgs &a, int64_t m, int 
     else if constexpr (OUT == kOutOp)
         op_store4(a.out_op, (int)m, col, a.op_folded, r);
     else
-        *reinterpret_cast<f32x4 *>(a.part_o + ((m * a.h_q + head) * a.splits + split) * a.d_h + d) = r;
+        *reinterpret_cast<f32x4 *>(a.part_o + ((m * a.h_q + head) * a.plan.splits + split) * a.d_h + d) = r;
 }
 
 // The scales of 64 blocks, one a lane, and from there to the block that asks: scalar loads would come back among the LDS reads, in no
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, flo
     t.template init<QB>(a, (int64_t)b * a.R + row, head, qi < NQ ? len + row : -1, g, scale_log2);
     const int seen = min(len + min(q0 + 15, NQ - 1) / group + 1, n_keys), all_see = len + q0 / group + 1;      // by some, by every row of the block
     const int n_blocks = (seen + kKv8Block - 1) / kKv8Block;
-    const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
+    const int first = split * a.plan.range, last = split + 1 == a.plan.splits ? n_blocks : min(n_blocks, first + a.plan.range);
     const size_t cache_row = (size_t)b * a.h_kv + hk;
     const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
     const size_t scale_row = cache_row * (a.max_len / kKv8Block);
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, flo
         const int64_t m = (int64_t)b * a.R + q / group;
         const int h = hk * group + q % group;
         store_out4<OUT>(a, m, h, split, d, r);
-        if (OUT == kOutPart && d == 0) a.part_ml[(m * a.h_q + h) * a.splits + split] = make_float2(M, L);
+        if (OUT == kOutPart && d == 0) a.part_ml[(m * a.h_q + h) * a.plan.splits + split] = make_float2(M, L);
     }
 }
 
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide
     const int block_seen = min(len + (int)by_group.div(min(c0 + QG * 32, NQ) - 1) + 1, n_keys);
     const int wave_seen = q0 < NQ ? min(len + (int)by_group.div(min(q0 + 32, NQ) - 1) + 1, n_keys) : 0;
     const int n_blocks = (block_seen + kKv8Block - 1) / kKv8Block;
-    const int first = split * a.range, last = split + 1 == a.splits ? n_blocks : min(n_blocks, first + a.range);
+    const int first = split * a.plan.range, last = split + 1 == a.plan.splits ? n_blocks : min(n_blocks, first + a.plan.range);
     const int whole = min(last, (len + (int)by_group.div(c0) + 1) / kKv8Block);            // blocks of keys below that every row of the block sees
     const size_t cache_row = (size_t)b * a.h_kv + hk;
     const uint8_t *K = a.k + cache_row * a.max_len * DH, *V = a.v + cache_row * a.max_len * DH;
@@ -624,7 +624,7 @@ __global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide
     l += __shfl_xor(l, 32, kWave);
     const float inv = l != 0.f ? vref / l : 0.f;             // (a split none of whose keys the row sees: 0; a sum that is no number is not 0)
     const int64_t mrow = (int64_t)b * a.R + row;
-    if (OUT == kOutPart && h == 0 && qi < NQ) a.part_ml[(mrow * a.h_q + head) * a.splits + split] = make_float2(m, l);
+    if (OUT == kOutPart && h == 0 && qi < NQ) a.part_ml[(mrow * a.h_q + head) * a.plan.splits + split] = make_float2(m, l);
     if constexpr (OUT == kOutOp) {
         if (qi >= NQ) return;
 #pragma unroll
@@ -662,7 +662,7 @@ __global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide
             if constexpr (OUT == kOutBf16) dst = (uint8_t *)(a.out_bf16 + mr * a.out_stride + hh * DH);
             else if constexpr (OUT == kOutF16) dst = (uint8_t *)(a.out16 + (mr * a.h_q + hh) * DH);
             else if constexpr (OUT == kOutF32) dst = (uint8_t *)(a.out + (mr * a.h_q + hh) * DH);
-            else dst = (uint8_t *)(a.part_o + ((mr * a.h_q + hh) * a.splits + split) * DH);
+            else dst = (uint8_t *)(a.part_o + ((mr * a.h_q + hh) * a.plan.splits + split) * DH);
             *reinterpret_cast<u32x4 *>(dst + piece * 16) = w;
         }
     }
@@ -674,13 +674,13 @@ __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
     const int64_t rh = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
     if (rh >= (int64_t)a.B * a.R * a.h_q) return;
     const int d = threadIdx.x % kLanes * 4;
-    const float2 *ml = a.part_ml + rh * a.splits;
-    const float *o = a.part_o + rh * a.splits * DH + d;
+    const float2 *ml = a.part_ml + rh * a.plan.splits;
+    const float *o = a.part_o + rh * a.plan.splits * DH + d;
     float M = ml[0].x;
-    for (int s = 1; s < a.splits; ++s) M = fmaxf(M, ml[s].x);
+    for (int s = 1; s < a.plan.splits; ++s) M = fmaxf(M, ml[s].x);
     float L = 0.f;
     f32x4 r{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
+    for (int s = 0; s < a.plan.splits; ++s) {
         const float2 e = ml[s];
         const float w = e.y * __builtin_amdgcn_exp2f(e.x - M);
         L += w;
@@ -691,42 +691,55 @@ __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
 
 }  // namespace
 
-// Query rows of a KV head that go to a block: up to 16 the direct kernel's, above the wide kernel's
-inline int wide_rows(int NQ) { return NQ > 64 ? 128 : NQ > 16 ? 64 : 16; }
-
-// Splits of the keys, so that few rows fill the chip.  Direct kernel: none up to 16 blocks of keys, four for each wavefront (one launch
-// instead of two); then one for four blocks up to eight splits, and up to sixteen on longer caches, while there is a CU for each
-// block of the grid; where the heads alone take more than half of the CUs, as many as are resident, but only on long caches.  us with
-// the join, by splits: 8 heads, 16 blocks 1: 9.5, 4: 9.2; 32 blocks 4: 10.9, 8: 10.6; 63 blocks 4: 12.7, 8: 11.5, 16: 13.2; 501 blocks 8: 31.6,
-// 16: 24.1, 32: 25.9; 64 heads, 63 blocks 4: 17.5, 8: 19.8; 251 blocks 4: 45.6, 8: 47.6; 160 heads, 32 blocks 1: 17.2, 3: 20.1; 126 blocks 1: 68, 3: 58;
-// 256 heads, 63 blocks 1: 41.6, 2: 45.7.
+// Splits of the keys, so that few rows fill the chip.
+// Direct kernel: none up to 16 blocks of keys, four for each wavefront (one launch instead of two); then one for four blocks up to eight
+// splits, and up to sixteen on longer caches, while there is a CU for each block of the grid; where the heads alone take more than half of
+// the CUs, as many as are resident, but only on long caches.  us with the join, by splits: 8 heads, 16 blocks 1: 9.5, 4: 9.2; 32 blocks 4: 10.9,
+// 8: 10.6; 63 blocks 4: 12.7, 8: 11.5, 16: 13.2; 501 blocks 8: 31.6, 16: 24.1, 32: 25.9; 64 heads, 63 blocks 4: 17.5, 8: 19.8; 251 blocks 4: 45.6, 8: 47.6;
+// 160 heads, 32 blocks 1: 17.2, 3: 20.1; 126 blocks 1: 68, 3: 58; 256 heads, 63 blocks 1: 41.6, 2: 45.7.
+static int direct_splits(long heads, int blocks) {           // heads: blocks of the grid without splits
+    if (blocks <= 16) return 1;
+    const long splits = heads > 128 && heads < 256 && blocks >= 96 ? 512 / heads : 256 / heads;
+    const int by_four = (blocks + 3) / 4, by_ten = blocks / 10 < 16 ? blocks / 10 : 16, most = by_four < 8 ? by_four : by_ten < 8 ? 8 : by_ten;
+    return splits < 1 ? 1 : splits < most ? (int)splits : most;
+}
 // Wide kernel: as many as there are CUs for, and twice that where each still walks 16 blocks, three blocks at least to a split.  us: 64 heads
 // (16 x 16 rows x 7 query heads), 65 blocks 2: 51.2, 4: 35.5, 8: 37.4; 48 heads (24 x 5 x 8), 47 blocks 2: 27, 5: 17.1, 10: 18.5; 8 heads (9 rows x 4), 16 blocks 1: 25.5,
 // 5: 13.7, 16: 15.5; 251 blocks 16: 32.8, 32: 28.4; 128 (4 x 33 rows x 32 heads), 17 blocks 1: 27.7, 2: 21.4, 4: 22.3; 64 blocks 2: 49.3, 4: 43.6.
-int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
-    const int NQ = h_q / h_kv * R, rows = wide_rows(NQ), blocks = (len_bound + kKv8Block - 1) / kKv8Block;
-    const long heads = (long)B * h_kv * ((NQ + rows - 1) / rows);
-    long splits;
-    if (rows > 16) {
-        // rows see half of the step's own keys on average
-        const int seen = (len_bound - R / 2 + kKv8Block - 1) / kKv8Block, most = seen / 3;
-        splits = 256 / heads;
-        if (splits > 0 && seen / splits >= 16) splits = 512 / heads;
-        splits = splits > most ? most : splits;
-    } else {
-        if (blocks <= 16) return 1;
-        splits = heads > 128 && heads < 256 && blocks >= 96 ? 512 / heads : 256 / heads;
-        const int by_four = (blocks + 3) / 4, by_ten = blocks / 10 < 16 ? blocks / 10 : 16, most = by_four < 8 ? by_four : by_ten < 8 ? 8 : by_ten;
-        splits = splits > most ? most : splits;
-    }
+static int wide_splits(long heads, int blocks) {
+    long splits = 256 / heads;
+    if (splits > 0 && blocks / splits >= 16) splits = 512 / heads;
+    const int most = blocks / 3;
+    splits = splits < most ? splits : most;
     return splits < 1 ? 1 : (int)splits;
 }
+static long grid_heads(int B, int h_kv, int NQ, int rows) { return (long)B * h_kv * ((NQ + rows - 1) / rows); }
+static int wide_rows(int NQ) { return NQ > 64 ? 128 : 64; }
 
-int kv8_attn_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound, int *range) {
-    const int blocks = (len_bound + kKv8Block - 1) / kKv8Block, splits = kv8_attn_max_splits(B, R, h_q, h_kv, d_h, len_bound);
-    const int r = (blocks + splits - 1) / splits;
-    if (range) *range = r;
-    return (blocks + r - 1) / r;
+// Query rows of a block.  16, the direct kernel's, while all its blocks are resident and few keys are walked again for every 16 rows: it
+// begins and ends sooner (no barrier, no LDS on the way in).  Above, the wide kernel turns codes once for 32 rows and reads them from LDS.  us, direct / wide: 8 heads x
+// 3 chunks of 16 rows, 5 blocks of keys 7.3 / 13.1; 63 blocks 12.5 / 22.4; 251 blocks 24.9 / 27.7; 128 grid blocks, 32 blocks of keys 17.3 / 18.5; 126 blocks 44.5 / 35.5; 192,
+// 32 blocks 19.2 / 20.0; 128, 64 blocks 26.5 / 21.7; 384, 6 blocks 11.1 / 13.5; 17 blocks 21.7 / 20.4; 768, 5 blocks 20.2 / 14.1; 64-wide heads, 256, 47 blocks 17.9 / 21.2.
+static bool direct(int B, int h_kv, int NQ, int d_h, int blocks) {
+    const long heads = grid_heads(B, h_kv, NQ, 16);
+    return NQ <= 16 || (heads <= 512 && heads * blocks * d_h <= 6200l * 128);
+}
+
+int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
+    const int NQ = h_q / h_kv * R, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
+    const int d = direct_splits(grid_heads(B, h_kv, NQ, 16), blocks), w = NQ > 16 ? wide_splits(grid_heads(B, h_kv, NQ, wide_rows(NQ)), blocks) : 1;
+    return d > w ? d : w;
+}
+
+Kv8AttnPlan kv8_attn_plan(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
+    const int NQ = h_q / h_kv * R, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
+    const int seen = (len_bound - R / 2 + kKv8Block - 1) / kKv8Block;                      // rows see half of the step's own keys on average
+    Kv8AttnPlan p;
+    p.rows = direct(B, h_kv, NQ, d_h, seen) ? 16 : wide_rows(NQ);
+    const int splits = p.rows == 16 ? direct_splits(grid_heads(B, h_kv, NQ, 16), blocks) : wide_splits(grid_heads(B, h_kv, NQ, p.rows), seen);
+    p.range = (blocks + splits - 1) / splits;
+    p.splits = (blocks + p.range - 1) / p.range;
+    return p;
 }
 
 void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
@@ -752,15 +765,15 @@ void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
                 const auto kernel = attn8_wide_kernel<DH, QG, KG, QB, OUT>;
                 if (lds > 64 * 1024)                         // more than a kernel gets unasked
                     (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-                launch_kernel(kernel, dim3(a.B * a.h_kv, a.splits, (NQ + QG * 32 - 1) / (QG * 32)), QG * KG * 64, lds, stream, a, scale_log2, FastDiv(a.h_q / a.h_kv));
+                launch_kernel(kernel, dim3(a.B * a.h_kv, a.plan.splits, (NQ + QG * 32 - 1) / (QG * 32)), QG * KG * 64, lds, stream, a, scale_log2, FastDiv(a.h_q / a.h_kv));
             };
-            if (wide_rows(NQ) == 128) wide(Int<4>{}, Int<1>{});
-            else if (wide_rows(NQ) == 64) wide(Int<2>{}, Int<2>{});
+            if (a.plan.rows == 128) wide(Int<4>{}, Int<1>{});
+            else if (a.plan.rows == 64) wide(Int<2>{}, Int<2>{});
             else
-                launch_kernel(attn8_direct_kernel<DH, QB, OUT>, dim3(a.splits, (NQ + 15) / 16, a.B * a.h_kv), 256, 0, stream, a, scale_log2);
+                launch_kernel(attn8_direct_kernel<DH, QB, OUT>, dim3(a.plan.splits, (NQ + 15) / 16, a.B * a.h_kv), 256, 0, stream, a, scale_log2);
         };
         by_head([&](auto dh) {
-            if (a.splits > 1) {
+            if (a.plan.splits > 1) {
                 if (a.q_bf16) go(dh, Int<1>{}, Int<kOutPart>{});
                 else go(dh, Int<0>{}, Int<kOutPart>{});
             } else if (a.q_bf16) {
@@ -772,7 +785,7 @@ void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
             }
         });
     }
-    if (a.splits > 1) {
+    if (a.plan.splits > 1) {
         ScopedProf sp(PSD_KIND_ATTN_COMBINE, stream);
         const int64_t rows = (int64_t)a.B * a.R * a.h_q, per = 256 / (a.d_h / 4);
         const unsigned grid = (unsigned)((rows + per - 1) / per);

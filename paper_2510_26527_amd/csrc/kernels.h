@@ -285,6 +285,10 @@ struct Kv8Source {
     int64_t slot_stride;
 };
 void launch_kv8_append(const Kv8AppendArgs &a, const Kv8Source &src, hipStream_t stream);
+struct Kv8AttnPlan {
+    int rows;                     // query rows of a block: 16 by the direct kernel, 64 or 128 by the wide one
+    int splits, range;            // splits of the keys, and the keys of one in blocks of 64
+};
 struct Kv8AttnArgs {
     const void *q;                // [B][R][h_q][d_h] rotated queries, rows q_stride elements apart
     int64_t q_stride;
@@ -294,7 +298,7 @@ struct Kv8AttnArgs {
     const int32_t *lens;          // [B] valid positions BEFORE this step, whose rows are in the cache already
     int B, R, h_q, h_kv, d_h, max_len;
     float scale;                  // of the scores
-    int splits, range;            // kv8_attn_plan: keys of a split, in blocks of 64
+    Kv8AttnPlan plan;
     uint16_t *out_bf16;           // one of the four, rows out_stride elements apart where it says so
     int64_t out_stride;
     float *out;                   // [B][R][h_q * d_h]
@@ -303,7 +307,7 @@ struct Kv8AttnArgs {
     float *part_o;                // [B][R][h_q][splits][d_h], a split's normalised result
     float2 *part_ml;              // [B][R][h_q][splits] (reference, sum of weights)
 };
-int kv8_attn_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound, int *range);
+Kv8AttnPlan kv8_attn_plan(int B, int R, int h_q, int h_kv, int d_h, int len_bound);
 int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound);      // of any cache up to len_bound
 void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream);
 

@@ -262,7 +262,10 @@ def _room(ref, weighted):
 ATTN_CASES = [  # B, R, h_q, h_kv, d, lens (before the rows)
     (1, 1, 1, 1, 64, [0]), (1, 1, 8, 2, 128, [0]), (2, 1, 8, 2, 128, [63, 64]), (1, 9, 4, 4, 128, [1024]), (3, 5, 8, 2, 64, [0, 1, 700]),
     (2, 16, 7, 1, 128, [130, 5]), (1, 33, 4, 1, 128, [95]), (1, 200, 2, 2, 64, [0]), (1, 130, 4, 2, 128, [61]), (4, 3, 28, 4, 128, [0, 63, 65, 3000]),
-    (1, 1, 32, 8, 128, [5000]), (2, 70, 14, 2, 128, [0, 260]), (1, 300, 3, 1, 128, [0]), (1, 2, 16, 1, 64, [129]), (9, 17, 2, 1, 64, [7 * i for i in range(9)])]
+    (1, 1, 32, 8, 128, [5000]), (2, 70, 14, 2, 128, [0, 260]), (1, 1, 4, 1, 64, [9000]),
+    # many rows or many keys for them: blocks of 128 rows without and with splits of the keys, of 64 rows likewise
+    (3, 250, 12, 6, 64, [0, 100, 37]), (2, 170, 32, 16, 128, [70, 3]), (1, 100, 16, 4, 128, [4000]), (9, 12, 32, 8, 128, [2000 - 61 * i for i in range(9)]),
+    (17, 20, 16, 16, 128, [3 * i for i in range(17)]), (6, 40, 32, 32, 64, [1200, 0, 64, 63, 1199, 500]), (1, 300, 3, 1, 128, [0]), (1, 2, 16, 1, 64, [129]), (9, 17, 2, 1, 64, [7 * i for i in range(9)])]
 
 
 @pytest.mark.parametrize("case", ATTN_CASES, ids=[f"{c[0]}x{c[1]}-{c[2]}/{c[3]}x{c[4]}-{max(c[5])}" for c in ATTN_CASES])
@@ -285,25 +288,27 @@ def test_attention(case):
     assert torch.equal(free, runtime.KV8Attention()(c.layer, q.cuda()))
 
 
-@pytest.mark.parametrize("R", [1, 5, 40, 150])
-def test_what_a_row_does_not_see_has_no_part_in_it(R):
+@pytest.mark.parametrize("R,h_kv,group,d", [(1, 1, 4, 128), (5, 1, 4, 128), (40, 1, 4, 128), (150, 1, 4, 64),
+                                            (150, 8, 4, 128), (20, 130, 1, 64), (20, 130, 1, 128)])        # the last three: blocks of 128 and of 64 rows
+def test_what_a_row_does_not_see_has_no_part_in_it(R, h_kv, group, d):
     """Later rows of the step, and everything behind it, may hold NaN; a row that sees one gets NaN in V's entries, or all over for K."""
-    lens, d, B = [70, 200], 128, 2
-    c = Cache(B, 1, d, 448, [n + R for n in lens], seed=R)
+    lens, B = [70, 200], 2
+    c = Cache(B, h_kv, d, 448, [n + R for n in lens], seed=R)
     c.lens.copy_(torch.tensor(lens))
-    q = _randn(9, B, R, 4, d).to(BF16).cuda()
+    q = _randn(9, B, R, group * h_kv, d).to(BF16).cuda()
     attend = runtime.KV8Attention()
     clean = attend(c.layer, q, len_upper_bound=448)
     first = R // 2                                           # sequence 0: row `first` on sees a NaN value in entry 3
     c.layer.v[0, 0, (70 + first) // 64, 3, (70 + first) % 64] = 127
     got = attend(c.layer, q, len_upper_bound=448)
     assert torch.equal(got[1], clean[1]) and torch.equal(got[0, :first], clean[0, :first])
-    assert torch.isnan(got[0, first:, :, 3]).all() and torch.isnan(got).sum().item() == (R - first) * 4
+    assert torch.isnan(got[0, first:, :group, 3]).all() and torch.isnan(got).sum().item() == (R - first) * group
     rest = [e for e in range(d) if e != 3]
-    assert torch.equal(got[0][:, :, rest], clean[0][:, :, rest])
+    assert torch.equal(got[0][:, :, rest], clean[0][:, :, rest]) and torch.equal(got[0][:, group:], clean[0][:, group:])
     c.layer.k[1, 0, 200 + R - 1, 5] = 255                    # sequence 1: the last row sees a NaN key
     got = attend(c.layer, q, len_upper_bound=448)
-    assert torch.equal(got[1, :R - 1], clean[1, :R - 1]) and torch.isnan(got[1, R - 1]).all()
+    assert torch.equal(got[1, :R - 1], clean[1, :R - 1]) and torch.isnan(got[1, R - 1, :group]).all()
+    assert torch.equal(got[1, :, group:], clean[1, :, group:])
 
 
 def test_attention_scores_far_apart_and_scales_far_apart():
@@ -328,7 +333,7 @@ def test_attention_scores_far_apart_and_scales_far_apart():
         assert np.all(np.abs(got.double().cpu().numpy() - ref) <= _room(ref, weighted))
 
 
-@pytest.mark.parametrize("heads,R", [(1, 3), (2, 40), (5, 60)])
+@pytest.mark.parametrize("heads,R", [(1, 3), (2, 40), (5, 60), (64, 140)])            # the last: blocks of 128 rows
 @pytest.mark.parametrize("d", [64, 128])
 def test_attention_of_large_scores(heads, R, d):
     """Scores of 2^20 and 2^100, all equal or far apart: weights of 1 and 0."""
@@ -427,7 +432,7 @@ class Following(kv8.KVCache8):
     2^-3 of the entry apart, which later rows see in full; nothing bounds such a logit by 2e-2."""
 
     def __init__(self, cfg, batch, max_len, kv):
-        super().__init__(cfg, batch, max_len)
+        ofwd.KVCache.__init__(self, cfg, batch, max_len)     # (the codes are the GPU's)
         self.kv = kv
 
     def append(self, l, b, s0, k, v):
@@ -482,6 +487,44 @@ def test_forwards_on_an_8_bit_cache(shape, pack, w4):
             psd.psd_kv_truncate(kv.handle, base, keep, 0)
             okv.truncate(okv.lens - n + np.array([n - 1, n // 2]))
             assert kv.lens.tolist() == okv.lens.tolist()
+    kv.close()
+    model.close()
+
+
+def test_a_long_prompt_on_an_8_bit_cache():
+    """More rows than the direct kernel takes: the wide kernel's fp16 output, for the tiled projections."""
+    shape, B = synth.Shape(1, 256, 8, 4, 64, 256, 128, 1.0e4), 2
+    model = runtime.Model(shape, synth.make_weights(shape, 2, BF16, std=0.05)).pack()
+    w, cfg = {k: v.cpu() for k, v in model.weights.items()}, ofwd.ModelConfig(**shape.asdict())
+    kv = runtime.KVCache8(model, B, 704, fill_garbage=True)
+    okv = Following(cfg, B, 704, kv)
+    toks = synth.make_tokens(shape.vocab, (B, 660), 4)
+    for n in (620, 40):
+        t = toks[:, int(okv.lens[0]):int(okv.lens[0]) + n]
+        got = runtime.forward(model, kv, torch.from_numpy(t).cuda())
+        _logits_close(got, ofwd.forward(cfg, w, t, okv), f"{n} rows")
+    kv.close()
+    model.close()
+
+
+@pytest.mark.parametrize("pack", [False, True])
+def test_a_verify_step_on_a_long_8_bit_cache(pack):
+    """36 query rows a KV head on 17 000 keys: the wide kernel's splits and its outputs for steps of up to 16 rows."""
+    shape, ctx = synth.Shape(1, 512, 32, 8, 128, 256, 320, 5.0e5), 17000
+    model = runtime.Model(shape, synth.make_weights(shape, 2, BF16, std=0.05))
+    if pack:
+        model.pack()
+    w, cfg = {k: v.cpu() for k, v in model.weights.items()}, ofwd.ModelConfig(**shape.asdict())
+    kv = runtime.KVCache8(model, 1, 17088)
+    okv = Following(cfg, 1, 17088, kv)
+    ks, vs = synth.make_kv_fill(shape, 1, ctx, 6, BF16)
+    kv.load(ks, vs, ctx)
+    okv.append(0, 0, 0, ofwd.widen(ks[0][0]).transpose(1, 0, 2), ofwd.widen(vs[0][0]).transpose(1, 0, 2))
+    okv.lens[:] = ctx
+    toks = synth.make_tokens(shape.vocab, (1, 10), 9)
+    for n in (9, 1):
+        got = runtime.forward(model, kv, torch.from_numpy(toks[:, :n]).cuda())
+        _logits_close(got, ofwd.forward(cfg, w, toks[:, :n], okv), f"{n} rows")
     kv.close()
     model.close()
 
