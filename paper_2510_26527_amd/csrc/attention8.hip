@@ -667,24 +667,41 @@ __global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide
         }
     }
 }
-// Joins the splits of a row and head, in their order: 64 / (d_h / 4) of them a wavefront, four entries a lane.
+// Joins the splits of a row and head, in their order: 256 / d_h rows and heads a wavefront, four entries a lane.
 template <int DH, int OUT>
 __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
     constexpr int kLanes = DH / 4, kRows = 256 / kLanes;
     const int64_t rh = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
     if (rh >= (int64_t)a.B * a.R * a.h_q) return;
     const int d = threadIdx.x % kLanes * 4;
-    const float2 *ml = a.part_ml + rh * a.plan.splits;
-    const float *o = a.part_o + rh * a.plan.splits * DH + d;
-    float M = ml[0].x;
-    for (int s = 1; s < a.plan.splits; ++s) M = fmaxf(M, ml[s].x);
-    float L = 0.f;
+    const int S = a.plan.splits;
+    const float2 *ml = a.part_ml + rh * S;
+    const float *o = a.part_o + rh * S * DH + d;
+    float M = kFarBelow, L = 0.f;
     f32x4 r{0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.plan.splits; ++s) {
-        const float2 e = ml[s];
-        const float w = e.y * __builtin_amdgcn_exp2f(e.x - M);
-        L += w;
-        r += *reinterpret_cast<const f32x4 *>(o + (size_t)s * DH) * w;
+    constexpr int kTogether = 8;                             // loads in flight: up to eight splits are one trip to memory
+    for (int s0 = 0; s0 < S; s0 += kTogether) {
+        float2 e[kTogether];
+        f32x4 v[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            const int s = min(s0 + k, S - 1);
+            e[k] = ml[s];
+            v[k] = *reinterpret_cast<const f32x4 *>(o + (size_t)s * DH);
+        }
+        float top = M;
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) top = fmaxf(top, e[k].x);
+        const float shrink = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        L *= shrink;
+        r *= shrink;
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            const float w = s0 + k < S ? e[k].y * __builtin_amdgcn_exp2f(e[k].x - M) : 0.f;
+            L += w;
+            if (s0 + k < S) r += v[k] * w;
+        }
     }
     store_out4<OUT>(a, rh / a.h_q, (int)(rh % a.h_q), 0, d, r * (1.0f / L));
 }
