@@ -157,7 +157,7 @@ psd_status psd_rope_destroy(psd_rope *rope);
 psd_status psd_rope_frequencies(const psd_rope *rope, double *out_host);
 /* Turns the heads of `rows` rows: x, y device [rows][n_heads][d_head] of `dtype`, rows x_row_stride / y_row_stride elements
  * apart, heads dense; positions device int32[rows].  y may be x (the strides then equal); otherwise no element of y may be one of x.
- * Query and key heads that lie side by side in a row are one call.  rows = 0 is a no-op. */
+ * Query and key heads that lie side by side in a row are one call.  rows <= 2^23; rows = 0 is a no-op. */
 psd_status psd_rope_rotate(const psd_rope *rope, const void *x, void *y, const int32_t *positions, int32_t rows, int32_t n_heads,
                            int32_t dtype, int64_t x_row_stride, int64_t y_row_stride, void *hip_stream);
 /* Forwards of m turn by `rope` (copied; NULL: by the descriptor's rope_theta again) instead.  Its d_head must be the model's.

@@ -890,7 +890,7 @@ psd_status psd_rope_rotate(const psd_rope *rope, const void *x, void *y, const i
                            int32_t dtype, int64_t x_row_stride, int64_t y_row_stride, void *hip_stream) {
     if (!rope) return PSD_ERR_NULL;
     if (dtype != PSD_F32 && dtype != PSD_BF16) return PSD_ERR_DTYPE;
-    if (rows < 0 || n_heads <= 0 || n_heads > 65535) return PSD_ERR_SHAPE;
+    if (rows < 0 || rows > (1 << 23) || n_heads <= 0 || n_heads > 65535) return PSD_ERR_SHAPE;
     if (rows == 0) return PSD_OK;
     if (!x || !y || !positions) return PSD_ERR_NULL;
     const int64_t width = (int64_t)n_heads * rope->d_head;
@@ -941,6 +941,7 @@ psd_status psd_kv8_append(const psd_kv8_view *cache, const psd_rope *rope, const
     if (q && (q_row_stride < q_width || q_out_row_stride < q_width || (q == q_out && q_row_stride != q_out_row_stride))) return PSD_ERR_SHAPE;
     const size_t es = elem_size(dtype);
     if ((uintptr_t)q % es || (uintptr_t)k % es || (uintptr_t)v % es || (uintptr_t)q_out % es) return PSD_ERR_SHAPE;
+    if (kv8_append_grid(cache->batch, n_new, q ? n_q_heads : 0, cache->n_kv_heads, cache->d_head) >= 1L << 24) return PSD_ERR_SHAPE;       // 2^32 threads
     Kv8AppendArgs a{};
     a.k_codes = (uint8_t *)cache->k_codes; a.v_codes = (uint8_t *)cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
     a.lens = cache->lens; a.q_out = q_out; a.q_out_stride = q_out_row_stride;

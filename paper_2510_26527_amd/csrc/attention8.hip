@@ -3,10 +3,11 @@
 //
 // The codes become fp16, exactly, two an instruction, in the registers they were loaded into; both products run on the fp16
 // matrix cores.  A block's 64 keys share their scales, so K's multiplies the scores (with the softmax scale and log2 e, one number a
-// query and block) and V's is the unit that the output accumulates in, which moves where a block's differs from the one before.
+// query and block), and V's rides in the weights: a weight is 2^(score - reference + kLift) * (V's scale / the unit the output accumulates in).
 // Roundings: a query row is divided by the power of two that brings its largest entry to 1 .. 2 and rounded to fp16 (bf16 entries
-// down to 2^-17 of the row's largest stay exact, smaller ones are off by 2^-25 of it at most); the softmax weights are rounded to fp16, held at 2^10
-// times their size against the reference so that what a long cache adds up stays above fp16's smallest; sums, references and outputs are fp32.
+// down to 2^-17 of the row's largest stay exact, smaller ones are off by 2^-25 of it at most); the weights are rounded to fp16, half a step
+// being 2^-12 of a weight, and the sum is of the rounded ones; kLift keeps weights down to 2^-21 of the reference's in fp16's normal range and
+// the smallest that is not lost at 2^-32, so that what a million far keys add up to is kept.  Sums, references and outputs are fp32.
 //
 // Operands without a transpose or LDS: a wavefront takes the scores of 64 keys as S^T = K q^T in four 16 x 16 tiles.  Row i of tile t
 // is key 16 (i / 4) + 4 t + i % 4, so that lane group g ends up with the scores of keys 16 g .. 16 g + 15 of its query: exactly the
@@ -87,7 +88,8 @@ __device__ __forceinline__ void store_out4(const Kv8AttnArgs &a, int64_t m, int 
 }
 
 // The scales of 64 blocks, one a lane, and from there to the block that asks: scalar loads would come back among the LDS reads, in no
-// order, so that every wait for those became a wait for a scale's trip to memory (prompt of 2001 rows xx us against xx).
+// order, so that every wait for those became a wait for a scale's trip to memory (a prompt of 2001 rows
+// 55 us against 53; with the fetch behind the next block's loads, which it then waits for, 64).
 struct Scales {
     const float *k, *v;
     int end, base;                // base: block of lane 0
@@ -344,9 +346,13 @@ constexpr int wide_lds() {
 // a group, in the order of the operands: a piece of 1 KB is what the 64 lanes read at once, sixteen codes each, and becomes two
 // operands.  Row x of K's tile t is key 32 t + 16 (x / 4 % 2) + 4 (x / 8) + x % 4, so that a lane's scores, of keys 32 t + 16 h .. + 15 for lane
 // half h, are in the order of V's pieces.
-// What bounds it: a wavefront's own chain of LDS reads, scores, maximum, weights and product (xx clocks a block of keys, of which 1024 are
-// matrix instructions), which two wavefronts a SIMD overlap.  Eight wavefronts, KG = 2, rather than two blocks of four a CU: the blocks of
-// a prompt's last rows, which walk most keys, are then walked at that rate to their end.
+// Two blocks of four wavefronts a CU.  KG: with up to 64 rows the second pair of wavefronts takes every other block of keys.
+// What bounds it: instruction issue and a wavefront's own chain.  A block of 64 keys and 32 rows is 1024 clocks of matrix instructions, some 1400 of
+// vector ones (128 conversions, 32 exponentials of 8.6 clocks each) and about 900 of waits for LDS, the maximum and the barrier: a wavefront
+// alone on its SIMD takes 2700 clocks, two of them 2100 each.  A prompt of 2001 rows of the 7B shape (32 heads) 50 us = 660 TFLOP/s, against 27 us
+// at the rate of a large matrix product; its longest blocks, 32 blocks of keys, run alone for the second half.  Tried and not faster (us, the same prompt at 54 in that
+// session): conversions once for the block, fp16 in LDS, 56; the next block's scores under this one's weights, three sets of LDS, 56; eight
+// wavefronts with KG = 2, one block a CU, 60; 64 rows a block 64; two blocks of keys to a barrier 54.5; matrix instructions at a higher wave priority 53.5.
 template <int DH, int QG, int KG, bool QB, int OUT>
 __global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide_kernel(Kv8AttnArgs a, float scale_log2, FastDiv by_group) {
     constexpr int JT = DH / 32, PIECES = 4 * JT, MINE = PIECES / QG;       // K: 2 JT pieces [t][j], V: 2 JT [dt][w]

@@ -284,6 +284,7 @@ struct Kv8Source {
     int slots;                    // > 0: fp32 partial sums, this many slots slot_stride elements apart, rows 16-byte aligned
     int64_t slot_stride;
 };
+long kv8_append_grid(int B, int R, int h_q, int h_kv, int d_h);        // blocks of the launch (h_q 0: no queries)
 void launch_kv8_append(const Kv8AppendArgs &a, const Kv8Source &src, hipStream_t stream);
 struct Kv8AttnPlan {
     int rows;                     // query rows of a block: 16 by the direct kernel, 64 or 128 by the wide one

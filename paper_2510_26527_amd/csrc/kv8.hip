@@ -346,16 +346,29 @@ __global__ __launch_bounds__(kThreads) void kv8_append_kernel(Kv8AppendArgs a, R
 
 }  // namespace
 
+// the append launch's division: rows of a block of queries (16 rows of 64 angles fill the LDS), blocks of a group of rows, blocks of keys and values
+struct AppendShape { int q_rows, q_parts; long units, blocks; };
+static AppendShape append_shape(int B, int R, int h_q, int h_kv, int d_h) {
+    const int per_row = h_q * (d_h / 16), per_block = kThreads * kQueryItems;
+    AppendShape s{1, 1, 2L * B * h_kv * ((R + kKv8Block - 2) / kKv8Block + 1), 0};         // at most so many blocks of tokens of one sequence
+    s.blocks = s.units;
+    if (!h_q) return s;
+    s.q_rows = per_row >= per_block ? 1 : per_block / per_row < 16 ? per_block / per_row : 16;
+    s.q_parts = (s.q_rows * per_row + per_block - 1) / per_block;
+    s.blocks += ((long)B * R + s.q_rows - 1) / s.q_rows * s.q_parts;
+    return s;
+}
+long kv8_append_grid(int B, int R, int h_q, int h_kv, int d_h) { return append_shape(B, R, h_q, h_kv, d_h).blocks; }
+
 void launch_kv8_append(const Kv8AppendArgs &args, const Kv8Source &src, hipStream_t stream) {
     Kv8AppendArgs a = args;
-    const int blocks = (a.R + kKv8Block - 2) / kKv8Block + 1;                              // at most, of one sequence
-    a.units = 2 * a.B * a.h_kv * blocks;
-    const int per_row = a.h_q * (a.d_h / 16), per_block = kThreads * kQueryItems;
-    a.q_rows = per_row >= per_block ? 1 : per_block / per_row < 16 ? per_block / per_row : 16;           // (16 rows of 64 angles fill the LDS)
-    a.q_parts = (a.q_rows * per_row + per_block - 1) / per_block;
-    a.per_row = FastDiv(per_row);
+    const AppendShape shape = append_shape(a.B, a.R, a.q_out ? a.h_q : 0, a.h_kv, a.d_h);
+    a.units = (int)shape.units;
+    a.q_rows = shape.q_rows;
+    a.q_parts = shape.q_parts;
+    a.per_row = FastDiv(a.h_q * (a.d_h / 16));
     a.by_r = FastDiv(a.R);
-    const unsigned grid = a.units + (a.q_out ? (a.B * a.R + a.q_rows - 1) / a.q_rows * a.q_parts : 0);
+    const unsigned grid = (unsigned)shape.blocks;
     const bool odd = a.rope.rot % 16 != 0;
     const int out_es = src.bf16 ? 2 : 4;
     a.q_vec = (uintptr_t)a.q_out % 16 == 0 && a.q_out_stride * out_es % 16 == 0;

@@ -278,10 +278,12 @@ class KV8Layer:
 
 
 class KV8Attention:
-    """Workspace of psd_kv8_attention, reused across calls (on one stream at a time)."""
+    """Workspace of psd_kv8_attention, reused across calls (on one stream at a time).  One that was outgrown is kept, since a captured
+    graph may point at it; each is at least twice its predecessor."""
 
     def __init__(self):
         self._ws = None
+        self._outgrown = []
 
     def __call__(self, cache: KV8Layer, q, scale=0.0, len_upper_bound=None, out=None, stream=None):
         """q bf16 [B, n_new, h_q, d_h], the rows just appended to `cache` -> bf16 of the same shape; scale 0: 1 / sqrt(d_h).
@@ -305,6 +307,9 @@ class KV8Attention:
                 if grown or e.status != psd.PSD_ERR_WORKSPACE:
                     raise
                 need = psd.psd_kv8_attention_workspace_bytes(B, n, h_q, view.n_kv_heads, d, bound)
+                if self._ws is not None:
+                    self._outgrown.append(self._ws)
+                    need = max(need, 2 * self._ws.numel())
                 self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
 
 

@@ -414,6 +414,11 @@ def test_append_and_attention_captured_and_replayed(stream):
         a.lens += R - turn % 2                               # a rejected row now and then
         b.lens += R - turn % 2
         torch.cuda.synchronize()
+        if turn == 1:                                        # the workspace is outgrown: the graph's stays its own
+            wide = Cache(2, 8, d, 1984, [1900, 1900], seed=3)
+            attend(wide.layer, torch.zeros((2, 4, 32, d), dtype=BF16, device="cuda"))
+            assert attend._outgrown
+            torch.full((1 << 24,), float("nan"), device="cuda")
 
 
 SMALL = synth.Shape(2, 256, 4, 2, 64, 512, 1024, 1.0e4)

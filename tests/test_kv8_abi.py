@@ -51,7 +51,7 @@ def test_rope_rotate_refusals():
     call = lambda **kw: L.psd_rope_rotate(*{**dict(rope=r, x=P[0], y=P[1], pos=P[2], rows=3, heads=2, dtype=0, xs=128, ys=128, st=None), **kw}.values())
     assert call(rope=None) == psd.PSD_ERR_NULL and call(x=None) == psd.PSD_ERR_NULL and call(pos=None) == psd.PSD_ERR_NULL
     assert call(dtype=2) == psd.PSD_ERR_DTYPE
-    for kw in (dict(rows=-1), dict(heads=0), dict(heads=65536), dict(xs=127), dict(ys=0), dict(y=P[0], ys=256), dict(x=P[0] + 2), dict(pos=P[2] + 1)):
+    for kw in (dict(rows=-1), dict(rows=(1 << 23) + 1), dict(heads=0), dict(heads=65536), dict(xs=127), dict(ys=0), dict(y=P[0], ys=256), dict(x=P[0] + 2), dict(pos=P[2] + 1)):
         assert call(**kw) == psd.PSD_ERR_SHAPE, kw
     assert call(rows=0, x=None, y=None, pos=None) == psd.PSD_OK
     psd.psd_rope_destroy(r)
@@ -137,6 +137,8 @@ def test_append_refusals():
                dict(k=P[6] + 1), dict(q_out=P[5], os=512)):
         assert call(**kw) == psd.PSD_ERR_SHAPE, kw
     assert call(ub=129) == psd.PSD_ERR_CAPACITY and call(ub=2) == psd.PSD_ERR_CAPACITY
+    big = _view(batch=64, n_kv_heads=1023, max_len=1 << 15)   # more blocks than a launch has
+    assert call(big, n=16384, h=1023, qs=1023 * 64, ks=1023 * 64, vs=1023 * 64, os=1023 * 64, ub=16384) == psd.PSD_ERR_SHAPE
     other = _rope(d_head=128)
     assert call(rope=other) == psd.PSD_ERR_SHAPE
     for kw, status in VIEW_REFUSALS:
