@@ -222,9 +222,9 @@ psd_status psd_kv8_append(const psd_kv8_view *cache, const psd_rope *rope, const
 /* out = softmax(scale * q K^T) V for the rows just appended: row r of sequence b sees positions 0 .. lens[b] + r (lens as
  * before the step).  Query head h reads KV head h / (n_q_heads / n_kv_heads).
  *   q, out    device bf16 [batch * n_new][n_q_heads][d_head], rows *_row_stride elements apart, both 16-byte aligned with strides
- *             a multiple of 8 (PSD_ERR_SHAPE); out may not overlap q
+ *             a multiple of 8 (PSD_ERR_SHAPE); out may not overlap q (out = q: PSD_ERR_SHAPE)
  *   scale     0: 1 / sqrt(d_head)
- *   workspace 256-byte aligned, psd_kv8_attention_workspace_bytes() of the same numbers (0 bytes: may be NULL)
+ *   workspace 256-byte aligned, psd_kv8_attention_workspace_bytes() of the same numbers (0: none needed, or the call refuses them)
  * Scales in the cache must be positive, finite and between 2^-40 and 2^40.  What lies at positions that a row does not
  * see has no part in its result, whatever it is.  Sums, softmax and outputs in fp32, weights rounded to fp16. */
 size_t psd_kv8_attention_workspace_bytes(int32_t batch, int32_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t d_head,

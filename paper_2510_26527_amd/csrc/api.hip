@@ -915,14 +915,18 @@ psd_status psd_kv8_layer(const psd_kv *kv, int32_t layer, psd_kv8_view *out) {
     return PSD_OK;
 }
 
+static bool kv8_shape_ok(int batch, int n_new, int n_q_heads, int n_kv_heads, int d_head) {
+    if (d_head != 64 && d_head != 128) return false;
+    if (batch <= 0 || n_kv_heads <= 0 || (long)batch * n_kv_heads > 65535) return false;
+    if (n_new <= 0 || n_q_heads <= 0 || n_q_heads > 1024 || n_q_heads % n_kv_heads) return false;
+    return (long)batch * n_new <= (1L << 20) && (long)(n_q_heads / n_kv_heads) * n_new <= (1L << 20);
+}
+
 // what both calls on a layer check alike
 static psd_status check_kv8(const psd_kv8_view *c, int n_new, int n_q_heads, int len_upper_bound) {
     if (!c || !c->k_codes || !c->v_codes || !c->k_scale || !c->v_scale || !c->lens) return PSD_ERR_NULL;
-    if (c->d_head != 64 && c->d_head != 128) return PSD_ERR_SHAPE;
-    if (c->batch <= 0 || c->n_kv_heads <= 0 || (long)c->batch * c->n_kv_heads > 65535) return PSD_ERR_SHAPE;
+    if (!kv8_shape_ok(c->batch, n_new, n_q_heads, c->n_kv_heads, c->d_head)) return PSD_ERR_SHAPE;
     if (c->max_len <= 0 || c->max_len % kKv8Block) return PSD_ERR_SHAPE;
-    if (n_new <= 0 || n_q_heads <= 0 || n_q_heads > 1024 || n_q_heads % c->n_kv_heads) return PSD_ERR_SHAPE;
-    if ((long)c->batch * n_new > (1L << 20) || (long)(n_q_heads / c->n_kv_heads) * n_new > (1L << 20)) return PSD_ERR_SHAPE;
     if ((uintptr_t)c->k_codes % 16 || (uintptr_t)c->v_codes % 16 || (uintptr_t)c->k_scale % 4 || (uintptr_t)c->v_scale % 4) return PSD_ERR_SHAPE;
     if (len_upper_bound < n_new || len_upper_bound > c->max_len) return PSD_ERR_CAPACITY;
     return PSD_OK;
@@ -963,7 +967,7 @@ static size_t kv8_attention_scratch(int B, int R, int h_q, int d_h, int splits, 
 
 size_t psd_kv8_attention_workspace_bytes(int32_t batch, int32_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t d_head,
                                          int32_t len_upper_bound) {
-    if (batch <= 0 || n_new <= 0 || n_kv_heads <= 0 || n_q_heads <= 0 || n_q_heads % n_kv_heads || len_upper_bound <= 0) return 0;
+    if (!kv8_shape_ok(batch, n_new, n_q_heads, n_kv_heads, d_head) || len_upper_bound <= 0 || len_upper_bound > INT32_MAX - kKv8Block) return 0;
     size_t ml = 0;
     return kv8_attention_scratch(batch, n_new, n_q_heads, d_head, kv8_attn_plan(batch, n_new, n_q_heads, n_kv_heads, d_head, len_upper_bound).splits, &ml);
 }
@@ -976,7 +980,7 @@ psd_status psd_kv8_attention(const psd_kv8_view *cache, const void *q, void *out
     if (s != PSD_OK) return s;
     const int64_t width = (int64_t)n_q_heads * cache->d_head;
     if (q_row_stride < width || out_row_stride < width || q_row_stride % 8 || out_row_stride % 8) return PSD_ERR_SHAPE;
-    if ((uintptr_t)q % 16 || (uintptr_t)out % 16 || !std::isfinite(scale)) return PSD_ERR_SHAPE;
+    if ((uintptr_t)q % 16 || (uintptr_t)out % 16 || q == out || !std::isfinite(scale)) return PSD_ERR_SHAPE;
     Kv8AttnArgs a{};
     a.q = q; a.q_stride = q_row_stride; a.q_bf16 = true;
     a.k = (const uint8_t *)cache->k_codes; a.v = (const uint8_t *)cache->v_codes; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;

@@ -165,3 +165,14 @@ def test_attention_refusals():
         assert call(**kw) == psd.PSD_ERR_WORKSPACE, kw
     for kw, status in VIEW_REFUSALS:
         assert call(_view(**{"max_len": 4096, **kw})) == status, kw
+
+
+@pytest.mark.parametrize("args", [(1, 2**31 - 1, 64, 32, 128, 4096), (2**31 - 1, 1, 8, 8, 128, 4096), (1, 9, 2**31 - 1, 1, 128, 4096), (1, 9, 32, 8, 96, 4096),
+                                  (1, 9, 32, 8, 0, 4096), (1, 9, 32, 8, -128, 4096), (1, 9, 32, 8, 128, 2**31 - 1), (1, 9, 32, 8, 128, 0), (1, 1 << 20, 32, 8, 128, 1 << 21)])
+def test_no_workspace_size_for_what_the_call_refuses(args):
+    assert psd.psd_kv8_attention_workspace_bytes(*args) == 0
+
+
+def test_attention_into_its_own_queries_is_refused():
+    L = psd.lib()
+    assert L.psd_kv8_attention(ctypes.byref(_view()), P[5], P[5], 3, 4, 0.0, 256, 256, 100, P[9], 1 << 20, None) == psd.PSD_ERR_SHAPE
