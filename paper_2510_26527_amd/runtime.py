@@ -51,7 +51,6 @@ class Model:
         """Turn by `rope` (a Rope, None: by the shape's rope_theta) in every forward from now on."""
         psd.psd_model_set_rope(self.handle, None if rope is None else rope.handle)
         self.rope = rope
-        self._ws = None
         return self
 
     def pack(self):
@@ -128,6 +127,21 @@ def _current(*tensors):
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
 
 
+def _code(dtype):
+    code = _CODE.get(dtype)
+    if code is None:
+        raise ValueError(f"float32 or bfloat16 expected, not {dtype}")
+    return code
+
+
+def _made_on(stream, make, *args, **kw):
+    """A new tensor for `stream` (None: the current one) to write: what its memory held before must be done with on that stream."""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream):
+        return make(*args, **kw)
+
+
 def _row_stride(t):
     """Elements between the rows of t [..., heads, d], whose heads are dense within a row, and rows evenly apart."""
     shape = t.shape
@@ -158,10 +172,16 @@ class Rope:
 
     def __init__(self, d_head, rot_dim=None, layout="half", theta=1.0e4, scaling="none", factor=1.0, low=1.0, high=4.0,
                  original_len=0, magnitude=1.0):
-        self.handle = None
+        self._handle = None
         self.d_head, self.rot_dim = d_head, d_head if rot_dim is None else rot_dim
-        self.handle = psd.psd_rope_create(psd.psd_rope_desc(d_head, self.rot_dim, self._LAYOUT[layout], self._SCALING[scaling], theta,
+        self._handle = psd.psd_rope_create(psd.psd_rope_desc(d_head, self.rot_dim, self._LAYOUT[layout], self._SCALING[scaling], theta,
                                                             factor, low, high, original_len, magnitude))
+
+    @property
+    def handle(self):
+        if self._handle is None:                             # (no handle would mean: nothing turns)
+            raise ValueError("this Rope was closed")
+        return self._handle
 
     def frequencies(self):
         return psd.psd_rope_frequencies(self.handle, self.rot_dim // 2)
@@ -172,19 +192,19 @@ class Rope:
         if shape[:-2] != positions.shape or shape[-1] != self.d_head or positions.dtype != torch.int32 or not positions.is_contiguous():
             raise ValueError("x [..., heads, d_head] with contiguous int32 positions [...] expected")
         if out is None:
-            out = torch.empty_like(x)
+            out = _made_on(stream, torch.empty_like, x)
         elif out.shape != shape or out.dtype != x.dtype:
             raise ValueError("out has another shape or type than x")
         _current(x, positions, out)
         rows = positions.numel()
         if rows:
-            psd.psd_rope_rotate(self.handle, x, out, positions, rows, shape[-2], _CODE[x.dtype], _row_stride(x), _row_stride(out), stream)
+            psd.psd_rope_rotate(self.handle, x, out, positions, rows, shape[-2], _code(x.dtype), _row_stride(x), _row_stride(out), stream)
         return out
 
     def close(self):
-        if self.handle is not None:
-            psd.psd_rope_destroy(self.handle)
-            self.handle = None
+        if self._handle is not None:
+            psd.psd_rope_destroy(self._handle)
+            self._handle = None
 
 
 class KVCache8:
@@ -267,19 +287,19 @@ class KV8Layer:
             if q.shape != (B, n, h_q, d) or q.dtype != k.dtype:
                 raise ValueError("q is [B, n_new, n_q_heads, d_head] of k's type")
             if q_out is None:
-                q_out = torch.empty_like(q)
+                q_out = _made_on(stream, torch.empty_like, q)
             elif q_out.shape != q.shape or q_out.dtype != q.dtype:
                 raise ValueError("q_out has another shape or type than q")
             _current(k, v, self.k, q, q_out)
             q_stride, out_stride = _row_stride(q), _row_stride(q_out)
-        psd.psd_kv8_append(view, None if rope is None else rope.handle, q, k, v, q_out, n, h_q, _CODE[k.dtype], q_stride,
+        psd.psd_kv8_append(view, None if rope is None else rope.handle, q, k, v, q_out, n, h_q, _code(k.dtype), q_stride,
                            _row_stride(k), _row_stride(v), out_stride, view.max_len if len_upper_bound is None else len_upper_bound, stream)
         return q_out
 
 
 class KV8Attention:
     """Workspace of psd_kv8_attention, reused across calls (on one stream at a time).  One that was outgrown is kept, since a captured
-    graph may point at it; each is at least twice its predecessor."""
+    graph may point at it; each is at least twice its predecessor (of the same device)."""
 
     def __init__(self):
         self._ws = None
@@ -293,12 +313,15 @@ class KV8Attention:
         if B != view.batch or d != view.d_head or q.dtype != torch.bfloat16:
             raise ValueError("q is bf16 [B, n_new, n_q_heads, d_head]")
         if out is None:
-            out = torch.empty_like(q)
+            out = _made_on(stream, torch.empty_like, q)
         elif out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError("out has another shape or type than q")
         _current(q, cache.k, out)
         bound = view.max_len if len_upper_bound is None else len_upper_bound
         q_stride, out_stride = _row_stride(q), _row_stride(out)
+        if self._ws is not None and self._ws.device != q.device:
+            self._outgrown.append(self._ws)
+            self._ws = None
         for grown in (False, True):
             try:
                 psd.psd_kv8_attention(view, q, out, n, h_q, scale, q_stride, out_stride, bound, self._ws, stream)
@@ -310,7 +333,7 @@ class KV8Attention:
                 if self._ws is not None:
                     self._outgrown.append(self._ws)
                     need = max(need, 2 * self._ws.numel())
-                self._ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+                self._ws = _made_on(stream, torch.empty, need, dtype=torch.uint8, device=q.device)
 
 
 def forward(model: Model, kv: KVCache, tokens, n_logit_rows=None, logits_out=None, stream=None):

@@ -636,3 +636,57 @@ def test_tensors_that_do_not_fit_are_refused_before_a_launch():
             r.rotate(*args)
     with pytest.raises(ValueError):
         runtime.KV8Layer(c.layer.k, c.layer.v.float(), c.layer.k_scale, c.layer.v_scale, c.lens)
+    for dtype in (torch.float16, torch.float64):
+        with pytest.raises(ValueError):
+            r.rotate(x.to(dtype), torch.zeros(2, 3, dtype=torch.int32, device="cuda"))
+        with pytest.raises(ValueError):
+            c.layer.append(None, x.to(dtype), x.to(dtype))
+
+
+@pytest.mark.parametrize("as_number", [False, True])
+def test_results_made_for_another_stream_take_no_memory_that_this_one_still_reads(as_number):
+    """Memory given back while the current stream has work on it pending is free for that stream alone."""
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream if as_number else side
+    B, R, h_q, h_kv, d = 1, 64, 32, 8, 128
+    c = Cache(B, h_kv, d, 2048, [1900], seed=2)
+    rope, _ = _rope(d, d, "half", "none")
+    q, k, v = (_randn(3 + i, B, R, h, d).to(BF16).cuda() for i, h in enumerate((h_q, h_kv, h_kv)))
+    pos = torch.arange(R, dtype=torch.int32, device="cuda")[None]
+    attend = runtime.KV8Attention()
+    torch.cuda.synchronize()
+    for make in (lambda: rope.rotate(q, pos, stream=stream), lambda: c.layer.append(q, k, v, rope, stream=stream),
+                 lambda: attend(c.layer, q, stream=stream)):
+        held = torch.full_like(q, 3.0)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        copy = held.clone()                                  # waits behind the sleep
+        del held
+        got = make()
+        torch.cuda.synchronize()
+        assert bool((copy == 3.0).all())
+        assert not bool((got == 3.0).all())
+
+
+def test_a_forward_on_an_8_bit_cache_captured_and_replayed():
+    """One graph of a step, replayed as the cache grows to twice the length it was planned for, against eager steps on a twin."""
+    model = runtime.Model(GROUPED, synth.make_weights(GROUPED, 6, BF16, std=0.05)).pack()
+    a, b = (runtime.KVCache8(model, 2, 512) for _ in range(2))
+    prompt = torch.from_numpy(synth.make_tokens(GROUPED.vocab, (2, 70), 1)).cuda()
+    logits = torch.zeros((2, 9, GROUPED.vocab), dtype=F32, device="cuda")
+    toks = torch.zeros((2, 9), dtype=torch.int32, device="cuda")
+    model.workspace_upto(2, 70, 512)
+    for kv in (a, b):
+        runtime.forward(model, kv, prompt, 0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        runtime.forward(model, a, toks, logits_out=logits)
+    for turn in range(8):
+        toks.copy_(torch.from_numpy(synth.make_tokens(GROUPED.vocab, (2, 9), 30 + turn)))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = runtime.forward(model, b, toks)
+        assert torch.equal(a.lens, b.lens) and torch.equal(logits, want)
+        torch.cuda.synchronize()
+    model.close()

@@ -3,9 +3,11 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import rotary
 import paper_2510_26527_amd as psd
+from paper_2510_26527_amd import runtime
 
 P = [0x100000 + 0x10000 * i for i in range(12)]               # addresses nothing reads
 
@@ -176,3 +178,35 @@ def test_no_workspace_size_for_what_the_call_refuses(args):
 def test_attention_into_its_own_queries_is_refused():
     L = psd.lib()
     assert L.psd_kv8_attention(ctypes.byref(_view()), P[5], P[5], 3, 4, 0.0, 256, 256, 100, P[9], 1 << 20, None) == psd.PSD_ERR_SHAPE
+
+
+def test_a_closed_rope_is_refused():
+    """Its missing handle would mean that nothing turns."""
+    rope = runtime.Rope(64)
+    rope.frequencies()
+    rope.close()
+    rope.close()
+    for use in (lambda: rope.handle, rope.frequencies):
+        with pytest.raises(ValueError):
+            use()
+
+
+def test_an_attention_objects_workspace_stays_on_its_device(monkeypatch):
+    """Tensors of another device than the last call's get a workspace there; the old one stays for graphs."""
+    used = []
+
+    def launch(view, q, out, n, h_q, scale, qs, os, bound, ws, stream):
+        if ws is None:
+            raise psd.PsdError(psd.PSD_ERR_WORKSPACE, "attention")
+        used.append(ws.device)
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)          # (what get_device() says of the host)
+    monkeypatch.setattr(psd, "psd_kv8_attention", launch)
+    layer = runtime.KV8Layer(torch.zeros(1, 2, 4096, 64, dtype=torch.uint8), torch.zeros(1, 2, 64, 64, 64, dtype=torch.uint8), torch.ones(1, 2, 64),
+                             torch.ones(1, 2, 64), torch.zeros(1, dtype=torch.int32))
+    attend = runtime.KV8Attention()
+    q = torch.zeros(1, 3, 4, 64, dtype=torch.bfloat16)
+    attend(layer, q)
+    old = attend._ws = torch.empty(1 << 20, dtype=torch.uint8, device="meta")
+    attend(layer, q)
+    assert [d.type for d in used] == ["cpu", "cpu"] and attend._outgrown[-1] is old
