@@ -143,7 +143,9 @@ struct QueryTile {
 };
 
 // Few query rows: the wavefronts of a block share its 16 query rows and take every fourth block of 64 keys each; their results are
-// joined in LDS, and those of a sequence's splits by the combine kernel.
+// joined in LDS, and those of a sequence's splits by the combine kernel.  What bounds it: bytes on long caches (4 sequences of 131 000 keys, 8 KV heads of 128: 180 us =
+// 6.0 TB/s), else the chain of load, scores, weights and products of a wavefront's blocks of keys
+// (one token on 389 keys 7 us, 24 x 5 rows of 64-wide heads on up to 3000 keys 11.6).  No LDS on the way in: a code is used by one wavefront only.
 template <int DH, bool QB, int OUT>
 __global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, float scale_log2) {
     constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64;
@@ -673,7 +675,8 @@ __global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide
         }
     }
 }
-// Joins the splits of a row and head, in their order: 256 / d_h rows and heads a wavefront, four entries a lane.
+// Joins the splits of a row and head, in their order: 256 / d_h rows and heads a wavefront, four entries a lane.  One trip to memory: 288 rows
+// of 5 splits 3.2 us, 7168 rows of 8 splits 6.3 (4.9 TB/s).
 template <int DH, int OUT>
 __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
     constexpr int kLanes = DH / 4, kRows = 256 / kLanes;
@@ -726,12 +729,12 @@ static int direct_splits(long heads, int blocks) {           // heads: blocks of
     const int by_four = (blocks + 3) / 4, by_ten = blocks / 10 < 16 ? blocks / 10 : 16, most = by_four < 8 ? by_four : by_ten < 8 ? 8 : by_ten;
     return splits < 1 ? 1 : splits < most ? (int)splits : most;
 }
-// Wide kernel: as many as there are CUs for, and twice that where each still walks 16 blocks, three blocks at least to a split.  us: 64 heads
-// (16 x 16 rows x 7 query heads), 65 blocks 2: 51.2, 4: 35.5, 8: 37.4; 48 heads (24 x 5 x 8), 47 blocks 2: 27, 5: 17.1, 10: 18.5; 8 heads (9 rows x 4), 16 blocks 1: 25.5,
+// Wide kernel: as many as there are CUs for, and twice that where each still walks 12 blocks, three blocks at least to a split.  us: 64 heads
+// (16 x 16 rows x 7 query heads), 65 blocks 2: 53.6, 4: 35.9, 8: 36.6; 126 blocks 4: 53.3, 8: 51.6; 48 heads (24 x 5 x 8), 47 blocks 2: 27, 5: 17.1, 10: 18.5; 8 heads (9 rows x 4), 16 blocks 1: 25.5,
 // 5: 13.7, 16: 15.5; 251 blocks 16: 32.8, 32: 28.4; 128 (4 x 33 rows x 32 heads), 17 blocks 1: 27.7, 2: 21.4, 4: 22.3; 64 blocks 2: 49.3, 4: 43.6.
 static int wide_splits(long heads, int blocks) {
     long splits = 256 / heads;
-    if (splits > 0 && blocks / splits >= 16) splits = 512 / heads;
+    if (splits > 0 && blocks / splits >= 24) splits = 512 / heads;
     const int most = blocks / 3;
     splits = splits < most ? splits : most;
     return splits < 1 ? 1 : (int)splits;

@@ -120,11 +120,15 @@ _CODE = {torch.float32: psd.PSD_F32, torch.bfloat16: psd.PSD_BF16}
 
 
 def _current(*tensors):
-    """The library enqueues on the current device: a tensor of another one is the caller's mistake."""
+    """The library enqueues on the current device: a tensor of another one is the caller's mistake.  -> the current device."""
     here = torch.cuda.current_device()
     for t in tensors:
         if t.get_device() != here:
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
+    return here
+
+
+_raw = torch._C._cuda_getCurrentRawStream                    # a device's current stream, without a Stream object
 
 
 def _code(dtype):
@@ -149,8 +153,6 @@ def _row_stride(t):
     if t.is_contiguous():
         return width
     strides = t.stride()
-    if len(shape) == 4 and strides[3] == 1 and strides[2] == shape[3] and strides[0] == strides[1] * shape[1]:
-        return strides[1]                                    # [B, R, heads, d] of a buffer of projections
     if strides[-1] != 1 or (shape[-2] > 1 and strides[-2] != shape[-1]):
         raise ValueError("a row's heads have to lie side by side")
     stride, span = None, 1
@@ -162,6 +164,12 @@ def _row_stride(t):
                 raise ValueError("rows have to be evenly apart")
             span *= shape[k]
     return width if stride is None else stride
+
+
+def _row_stride4(t, n, d):
+    """_row_stride of t [B, n, heads, d], first for one piece or the heads of a buffer of projections."""
+    s0, s1, s2, s3 = t.stride()
+    return s1 if s3 == 1 and s2 == d and s0 == s1 * n else _row_stride(t)
 
 
 class Rope:
@@ -195,10 +203,11 @@ class Rope:
             out = _made_on(stream, torch.empty_like, x)
         elif out.shape != shape or out.dtype != x.dtype:
             raise ValueError("out has another shape or type than x")
-        _current(x, positions, out)
+        here = _current(x, positions, out)
         rows = positions.numel()
         if rows:
-            psd.psd_rope_rotate(self.handle, x, out, positions, rows, shape[-2], _code(x.dtype), _row_stride(x), _row_stride(out), stream)
+            psd.psd_rope_rotate(self.handle, x, out, positions, rows, shape[-2], _code(x.dtype), _row_stride(x), _row_stride(out),
+                                _raw(here) if stream is None else stream)
         return out
 
     def close(self):
@@ -269,31 +278,34 @@ class KV8Layer:
         if tuple(lens.shape) != (B,) or lens.dtype != torch.int32 or not all(t.is_contiguous() and t.device == k.device for t in (k, v, k_scale, v_scale, lens)):
             raise ValueError("lens is int32 [B], and every tensor contiguous and on one device")
         self.k, self.v, self.k_scale, self.v_scale, self.lens = k, v, k_scale, v_scale, lens
+        self.dims = B, h, d
         self.view = psd.psd_kv8_view(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), lens.data_ptr(), B, h, d, n)
 
     def append(self, q, k, v, rope=None, len_upper_bound=None, q_out=None, stream=None):
         """Rows q [B, n_new, h_q, d_h] (or None), k and v [B, n_new, h_kv, d_h], all fp32 or all bf16, at positions lens[b] ..: rotated
         by `rope` and quantised into the cache -> the rotated queries.  len_upper_bound: a bound of lens[b] + n_new."""
-        shape, view = k.shape, self.view
+        shape, dtype = k.shape, k.dtype
         B, n, h, d = shape
-        if B != view.batch or h != view.n_kv_heads or d != view.d_head or v.shape != shape or v.dtype != k.dtype:
+        if (B, h, d) != self.dims or v.shape != shape or v.dtype != dtype:
             raise ValueError("k and v are [B, n_new, n_kv_heads, d_head] of one type")
         q_stride, out_stride, h_q = 0, 0, h
         if q is None:
             q_out = None
-            _current(k, v, self.k)
+            here = _current(k, v, self.k)
         else:
-            h_q = q.shape[2]
-            if q.shape != (B, n, h_q, d) or q.dtype != k.dtype:
+            q_shape = q.shape
+            h_q = q_shape[2]
+            if q_shape != (B, n, h_q, d) or q.dtype != dtype:
                 raise ValueError("q is [B, n_new, n_q_heads, d_head] of k's type")
             if q_out is None:
                 q_out = _made_on(stream, torch.empty_like, q)
-            elif q_out.shape != q.shape or q_out.dtype != q.dtype:
+            elif q_out.shape != q_shape or q_out.dtype != dtype:
                 raise ValueError("q_out has another shape or type than q")
-            _current(k, v, self.k, q, q_out)
-            q_stride, out_stride = _row_stride(q), _row_stride(q_out)
-        psd.psd_kv8_append(view, None if rope is None else rope.handle, q, k, v, q_out, n, h_q, _code(k.dtype), q_stride,
-                           _row_stride(k), _row_stride(v), out_stride, view.max_len if len_upper_bound is None else len_upper_bound, stream)
+            here = _current(k, v, self.k, q, q_out)
+            q_stride, out_stride = _row_stride4(q, n, d), _row_stride4(q_out, n, d)
+        psd.psd_kv8_append(self.view, None if rope is None else rope.handle, q, k, v, q_out, n, h_q, _code(dtype), q_stride,
+                           _row_stride4(k, n, d), _row_stride4(v, n, d), out_stride,
+                           self.view.max_len if len_upper_bound is None else len_upper_bound, _raw(here) if stream is None else stream)
         return q_out
 
 
@@ -308,23 +320,24 @@ class KV8Attention:
     def __call__(self, cache: KV8Layer, q, scale=0.0, len_upper_bound=None, out=None, stream=None):
         """q bf16 [B, n_new, h_q, d_h], the rows just appended to `cache` -> bf16 of the same shape; scale 0: 1 / sqrt(d_h).
         len_upper_bound: a bound of lens[b] + n_new."""
-        view = cache.view
-        B, n, h_q, d = q.shape
-        if B != view.batch or d != view.d_head or q.dtype != torch.bfloat16:
+        view, shape = cache.view, q.shape
+        B, n, h_q, d = shape
+        if B != cache.dims[0] or d != cache.dims[2] or q.dtype != torch.bfloat16:
             raise ValueError("q is bf16 [B, n_new, n_q_heads, d_head]")
         if out is None:
             out = _made_on(stream, torch.empty_like, q)
-        elif out.shape != q.shape or out.dtype != q.dtype:
+        elif out.shape != shape or out.dtype != torch.bfloat16:
             raise ValueError("out has another shape or type than q")
-        _current(q, cache.k, out)
+        here = _current(q, cache.k, out)
         bound = view.max_len if len_upper_bound is None else len_upper_bound
-        q_stride, out_stride = _row_stride(q), _row_stride(out)
-        if self._ws is not None and self._ws.device != q.device:
+        q_stride, out_stride = _row_stride4(q, n, d), _row_stride4(out, n, d)
+        if self._ws is not None and self._ws.get_device() != here:
             self._outgrown.append(self._ws)
             self._ws = None
+        queue = _raw(here) if stream is None else stream
         for grown in (False, True):
             try:
-                psd.psd_kv8_attention(view, q, out, n, h_q, scale, q_stride, out_stride, bound, self._ws, stream)
+                psd.psd_kv8_attention(view, q, out, n, h_q, scale, q_stride, out_stride, bound, self._ws, queue)
                 return out
             except psd.PsdError as e:                        # too small a workspace so far: nothing was enqueued
                 if grown or e.status != psd.PSD_ERR_WORKSPACE:

@@ -201,12 +201,19 @@ def test_an_attention_objects_workspace_stays_on_its_device(monkeypatch):
         used.append(ws.device)
 
     monkeypatch.setattr(torch.cuda, "current_device", lambda: -1)          # (what get_device() says of the host)
+    monkeypatch.setattr(runtime, "_raw", lambda device: 0)
     monkeypatch.setattr(psd, "psd_kv8_attention", launch)
     layer = runtime.KV8Layer(torch.zeros(1, 2, 4096, 64, dtype=torch.uint8), torch.zeros(1, 2, 64, 64, 64, dtype=torch.uint8), torch.ones(1, 2, 64),
                              torch.ones(1, 2, 64), torch.zeros(1, dtype=torch.int32))
     attend = runtime.KV8Attention()
     q = torch.zeros(1, 3, 4, 64, dtype=torch.bfloat16)
     attend(layer, q)
-    old = attend._ws = torch.empty(1 << 20, dtype=torch.uint8, device="meta")
+    class Elsewhere:
+        device = torch.device("meta")
+
+        def get_device(self):
+            return 3
+
+    old = attend._ws = Elsewhere()
     attend(layer, q)
     assert [d.type for d in used] == ["cpu", "cpu"] and attend._outgrown[-1] is old
