@@ -152,10 +152,10 @@ __global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, flo
     __shared__ float s_o[4][16][DH + 4];
     __shared__ float s_m[4][16], s_l[4][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x, b = blockIdx.z / a.h_kv, hk = blockIdx.z % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
+    const int split = blockIdx.x, chunk = blockIdx.z, b = blockIdx.y / a.h_kv, hk = blockIdx.y % a.h_kv, group = a.h_q / a.h_kv, NQ = group * a.R;
     const int len = min(max(a.lens[b], 0), a.max_len);
     const int n_keys = min(len + a.R, a.max_len);
-    const int q0 = blockIdx.y * 16, qi = q0 + i;             // query row qi: head qi % group of the step's row qi / group
+    const int q0 = chunk * 16, qi = q0 + i;             // query row qi: head qi % group of the step's row qi / group
     const int row = min(qi, NQ - 1) / group, head = hk * group + min(qi, NQ - 1) % group;
     QueryTile<DH> t;
     t.template init<QB>(a, (int64_t)b * a.R + row, head, qi < NQ ? len + row : -1, g, scale_log2);
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, flo
     for (int dt = 0; dt < DT; ++dt) *reinterpret_cast<f32x4 *>(&s_o[wave][i][dt * 16 + 4 * g]) = t.o[dt] * vref;
     __syncthreads();
     for (int x = tid; x < 16 * (DH / 4); x += 256) {
-        const int qc = x / (DH / 4), d = x % (DH / 4) * 4, q = blockIdx.y * 16 + qc;
+        const int qc = x / (DH / 4), d = x % (DH / 4) * 4, q = q0 + qc;
         if (q >= NQ) continue;
         const float M = fmaxf(fmaxf(s_m[0][qc], s_m[1][qc]), fmaxf(s_m[2][qc], s_m[3][qc]));
         float L = 0.f;
@@ -718,16 +718,26 @@ __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
 }  // namespace
 
 // Splits of the keys, so that few rows fill the chip.
-// Direct kernel: none up to 16 blocks of keys, four for each wavefront (one launch instead of two); then one for four blocks up to eight
-// splits, and up to sixteen on longer caches, while there is a CU for each block of the grid; where the heads alone take more than half of
-// the CUs, as many as are resident, but only on long caches.  us with the join, by splits: 8 heads, 16 blocks 1: 9.5, 4: 9.2; 32 blocks 4: 10.9,
-// 8: 10.6; 63 blocks 4: 12.7, 8: 11.5, 16: 13.2; 501 blocks 8: 31.6, 16: 24.1, 32: 25.9; 64 heads, 63 blocks 4: 17.5, 8: 19.8; 251 blocks 4: 45.6, 8: 47.6;
+// Direct kernel: none up to 12 blocks of keys, three for each wavefront (one launch instead of two).  Above, the walk shrinks with the splits and the
+// join grows with them, so that the best number goes with the root of the length, sqrt(2 blocks), at least one for four blocks and 48 at most, while
+// there is a CU for each block of the grid; where the heads alone take more than half of the CUs, as many as are resident, but only on long
+// caches.  A split's keys are a multiple of four blocks, one for each wavefront.  us with the join, by splits: 8 heads, 16 blocks 1: 9.5, 4: 9.2;
+// 4 heads, 63 blocks 8: 9.5, 16: 9.3, 32: 10.1; 126 blocks 8: 12.0, 16: 10.4, 32: 10.7; 501 blocks 16: 19.6, 32: 15.3, 64: 15.9; 2047 blocks 16: 52.6, 32: 32.3,
+// 48: 29.1, 64: 30.8; 8 heads, 2047 blocks 16: 58.1, 32: 46.3, 40: 58.2; 64 heads, 63 blocks 4: 17.5, 8: 19.8; 251 blocks 4: 45.6, 8: 47.6;
 // 160 heads, 32 blocks 1: 17.2, 3: 20.1; 126 blocks 1: 68, 3: 58; 256 heads, 63 blocks 1: 41.6, 2: 45.7.
-static int direct_splits(long heads, int blocks) {           // heads: blocks of the grid without splits
-    if (blocks <= 16) return 1;
-    const long splits = heads > 128 && heads < 256 && blocks >= 96 ? 512 / heads : 256 / heads;
-    const int by_four = (blocks + 3) / 4, by_ten = blocks / 10 < 16 ? blocks / 10 : 16, most = by_four < 8 ? by_four : by_ten < 8 ? 8 : by_ten;
-    return splits < 1 ? 1 : splits < most ? (int)splits : most;
+struct DirectSplits { int most, cus; };                      // heads: blocks of the grid without splits
+static DirectSplits direct_splits(long heads, int blocks) {
+    const int cus = (int)((heads > 128 && heads < 256 && blocks >= 96 ? 512 : 256) / heads), by_four = (blocks + 3) / 4;
+    int most = (int)sqrt(2.0 * blocks);
+    most = most < by_four ? most : by_four;
+    most = most < 48 ? most : 48;
+    return blocks <= 12 || cus <= 1 ? DirectSplits{1, 1} : DirectSplits{most < cus ? most : cus, cus};
+}
+static int direct_range(long heads, int blocks) {
+    const DirectSplits s = direct_splits(heads, blocks);
+    if (s.cus == 1) return blocks;
+    const int nearest = (blocks + 2 * s.most) / (4 * s.most) * 4, range = nearest < 4 ? 4 : nearest;
+    return (blocks + range - 1) / range <= s.cus ? range : ((blocks + s.most - 1) / s.most + 3) / 4 * 4;
 }
 // Wide kernel: as many as there are CUs for, and twice that where each still walks 12 blocks, three blocks at least to a split.  us: 64 heads
 // (16 x 16 rows x 7 query heads), 65 blocks 2: 53.6, 4: 35.9, 8: 36.6; 126 blocks 4: 53.3, 8: 51.6; 48 heads (24 x 5 x 8), 47 blocks 2: 27, 5: 17.1, 10: 18.5; 8 heads (9 rows x 4), 16 blocks 1: 25.5,
@@ -743,17 +753,22 @@ static long grid_heads(int B, int h_kv, int NQ, int rows) { return (long)B * h_k
 static int wide_rows(int NQ) { return NQ > 64 ? 128 : 64; }
 
 // Query rows of a block.  16, the direct kernel's, while all its blocks are resident and few keys are walked again for every 16 rows: it
-// begins and ends sooner (no barrier, no LDS on the way in).  Above, the wide kernel turns codes once for 32 rows and reads them from LDS.  us, direct / wide: 8 heads x
-// 3 chunks of 16 rows, 5 blocks of keys 7.3 / 13.1; 63 blocks 12.5 / 22.4; 251 blocks 24.9 / 27.7; 128 grid blocks, 32 blocks of keys 17.3 / 18.5; 126 blocks 44.5 / 35.5; 192,
-// 32 blocks 19.2 / 20.0; 128, 64 blocks 26.5 / 21.7; 384, 6 blocks 11.1 / 13.5; 17 blocks 21.7 / 20.4; 768, 5 blocks 20.2 / 14.1; 64-wide heads, 256, 47 blocks 17.9 / 21.2.
+// begins and ends sooner (no barrier, no LDS on the way in).  Above, the wide kernel turns codes once for 32 rows and reads them from LDS; up
+// to 32 rows half of its wavefronts and more have no rows of their own, so that it pays later.  us, direct / wide, by blocks of the grid x blocks of keys: 3 chunks of 16 rows,
+// 24 x 251 18.7 / 20.4, 24 x 344 21.4 / 23.5, 24 x 501 26.8 / 26.6, 96 x 63 19.0 / 18.8, 96 x 126 30.0 / 24.4, 384 x 23 21.3 / 22.7; 7, 112 x 74 20.4 / 22.2; 25,
+// 200 x 43 19.1 / 24.6; 11, 176 x 88 33.3 / 28.6; 2 chunks, 64 x 126 19.9 / 23.4, 64 x 251 30.4 / 33.4, 64 x 376 41.6 / 42.5, 256 x 94 38.8 / 41.9; 64-wide heads, 3 chunks,
+// 144 x 47 10.6 / 13.1, 144 x 94 18.0 / 18.6; 768 x 5 20.2 / 14.1.
 static bool direct(int B, int h_kv, int NQ, int d_h, int blocks) {
     const long heads = grid_heads(B, h_kv, NQ, 16);
-    return NQ <= 16 || (heads <= 512 && heads * blocks * d_h <= 6200l * 128);
+    return NQ <= 16 || (heads <= 512 && heads * blocks * d_h <= (NQ <= 32 ? 20000l : 9000l) * 128);
 }
 
 int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
     const int NQ = h_q / h_kv * R, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
-    const int d = direct_splits(grid_heads(B, h_kv, NQ, 16), blocks), w = NQ > 16 ? wide_splits(grid_heads(B, h_kv, NQ, wide_rows(NQ)), blocks) : 1;
+    const long heads = grid_heads(B, h_kv, NQ, 16);
+    const DirectSplits s = direct_splits(heads, blocks);
+    const int rounded = s.most + s.most / 2 + 1, d = rounded < s.cus ? rounded : s.cus;          // (six blocks a split become four)
+    const int w = NQ > 16 ? wide_splits(grid_heads(B, h_kv, NQ, wide_rows(NQ)), blocks) : 1;
     return d > w ? d : w;
 }
 
@@ -762,8 +777,12 @@ Kv8AttnPlan kv8_attn_plan(int B, int R, int h_q, int h_kv, int d_h, int len_boun
     const int seen = (len_bound - R / 2 + kKv8Block - 1) / kKv8Block;                      // rows see half of the step's own keys on average
     Kv8AttnPlan p;
     p.rows = direct(B, h_kv, NQ, d_h, seen) ? 16 : wide_rows(NQ);
-    const int splits = p.rows == 16 ? direct_splits(grid_heads(B, h_kv, NQ, 16), blocks) : wide_splits(grid_heads(B, h_kv, NQ, p.rows), seen);
-    p.range = (blocks + splits - 1) / splits;
+    if (p.rows == 16)
+        p.range = direct_range(grid_heads(B, h_kv, NQ, 16), blocks);
+    else {
+        const int splits = wide_splits(grid_heads(B, h_kv, NQ, p.rows), seen);
+        p.range = (blocks + splits - 1) / splits;
+    }
     p.splits = (blocks + p.range - 1) / p.range;
     return p;
 }
@@ -796,7 +815,7 @@ void launch_kv8_attention(const Kv8AttnArgs &a, hipStream_t stream) {
             if (a.plan.rows == 128) wide(Int<4>{}, Int<1>{});
             else if (a.plan.rows == 64) wide(Int<2>{}, Int<2>{});
             else
-                launch_kernel(attn8_direct_kernel<DH, QB, OUT>, dim3(a.plan.splits, (NQ + 15) / 16, a.B * a.h_kv), 256, 0, stream, a, scale_log2);
+                launch_kernel(attn8_direct_kernel<DH, QB, OUT>, dim3(a.plan.splits, a.B * a.h_kv, (NQ + 15) / 16), 256, 0, stream, a, scale_log2);
         };
         by_head([&](auto dh) {
             if (a.plan.splits > 1) {

@@ -265,7 +265,9 @@ ATTN_CASES = [  # B, R, h_q, h_kv, d, lens (before the rows)
     (1, 1, 32, 8, 128, [5000]), (2, 70, 14, 2, 128, [0, 260]), (1, 1, 4, 1, 64, [9000]),
     # many rows or many keys for them: blocks of 128 rows without and with splits of the keys, of 64 rows likewise
     (3, 250, 12, 6, 64, [0, 100, 37]), (2, 170, 32, 16, 128, [70, 3]), (1, 100, 16, 4, 128, [4000]), (9, 12, 32, 8, 128, [2000 - 61 * i for i in range(9)]),
-    (17, 20, 16, 16, 128, [3 * i for i in range(17)]), (6, 40, 32, 32, 64, [1200, 0, 64, 63, 1199, 500]), (1, 300, 3, 1, 128, [0]), (1, 2, 16, 1, 64, [129]), (9, 17, 2, 1, 64, [7 * i for i in range(9)])]
+    (17, 20, 16, 16, 128, [3 * i for i in range(17)]), (6, 40, 32, 32, 64, [1200, 0, 64, 63, 1199, 500]), (1, 300, 3, 1, 128, [0]), (1, 2, 16, 1, 64, [129]), (9, 17, 2, 1, 64, [7 * i for i in range(9)]),
+    (1, 100, 32, 8, 128, [4000]), (9, 12, 32, 8, 128, [4000 - 61 * i for i in range(9)]), (1, 11, 16, 4, 128, [8100]), (1, 1, 8, 2, 128, [17000]),
+    (5, 5, 16, 8, 64, [0, 900, 777, 1000, 63])]
 
 
 @pytest.mark.parametrize("case", ATTN_CASES, ids=[f"{c[0]}x{c[1]}-{c[2]}/{c[3]}x{c[4]}-{max(c[5])}" for c in ATTN_CASES])
@@ -512,16 +514,17 @@ def test_a_long_prompt_on_an_8_bit_cache():
     model.close()
 
 
+@pytest.mark.parametrize("ctx", [17000, 25000])
 @pytest.mark.parametrize("pack", [False, True])
-def test_a_verify_step_on_a_long_8_bit_cache(pack):
-    """36 query rows a KV head on 17 000 keys: the wide kernel's splits and its outputs for steps of up to 16 rows."""
-    shape, ctx = synth.Shape(1, 512, 32, 8, 128, 256, 320, 5.0e5), 17000
+def test_a_verify_step_on_a_long_8_bit_cache(pack, ctx):
+    """36 query rows a KV head: the direct kernel's and, on 25 000 keys, the wide kernel's splits and outputs for steps of up to 16 rows."""
+    shape = synth.Shape(1, 512, 32, 8, 128, 256, 320, 5.0e5)
     model = runtime.Model(shape, synth.make_weights(shape, 2, BF16, std=0.05))
     if pack:
         model.pack()
     w, cfg = {k: v.cpu() for k, v in model.weights.items()}, ofwd.ModelConfig(**shape.asdict())
-    kv = runtime.KVCache8(model, 1, 17088)
-    okv = Following(cfg, 1, 17088, kv)
+    kv = runtime.KVCache8(model, 1, ctx // 64 * 64 + 128)
+    okv = Following(cfg, 1, ctx // 64 * 64 + 128, kv)
     ks, vs = synth.make_kv_fill(shape, 1, ctx, 6, BF16)
     kv.load(ks, vs, ctx)
     okv.append(0, 0, 0, ofwd.widen(ks[0][0]).transpose(1, 0, 2), ofwd.widen(vs[0][0]).transpose(1, 0, 2))
@@ -530,6 +533,24 @@ def test_a_verify_step_on_a_long_8_bit_cache(pack):
     for n in (9, 1):
         got = runtime.forward(model, kv, torch.from_numpy(toks[:, :n]).cuda())
         _logits_close(got, ofwd.forward(cfg, w, toks[:, :n], okv), f"{n} rows")
+    kv.close()
+    model.close()
+
+
+@pytest.mark.parametrize("pack", [False, True])
+def test_a_small_step_of_many_heads_on_an_8_bit_cache(pack):
+    """52 KV heads of eight query heads, five sequences of three rows: the wide kernel without splits in a step of up to 16 rows."""
+    shape = synth.Shape(1, 256, 416, 52, 64, 256, 320, 1.0e4)
+    model = runtime.Model(shape, synth.make_weights(shape, 2, BF16, std=0.05))
+    if pack:
+        model.pack()
+    w, cfg = {k: v.cpu() for k, v in model.weights.items()}, ofwd.ModelConfig(**shape.asdict())
+    kv = runtime.KVCache8(model, 5, 128, fill_garbage=True)
+    okv = Following(cfg, 5, 128, kv)
+    toks = synth.make_tokens(shape.vocab, (5, 68), 9)
+    for at, n in ((0, 62), (62, 3), (65, 3)):
+        got = runtime.forward(model, kv, torch.from_numpy(toks[:, at:at + n]).cuda())
+        _logits_close(got, ofwd.forward(cfg, w, toks[:, at:at + n], okv), f"{n} rows")
     kv.close()
     model.close()
 
