@@ -6,7 +6,7 @@
 // query and block), and V's rides in the weights: a weight is 2^(score - reference + kLift) * (V's scale / the unit the output accumulates in).
 // Roundings: a query row is divided by the power of two that brings its largest entry to 1 .. 2 and rounded to fp16 (bf16 entries
 // down to 2^-17 of the row's largest stay exact, smaller ones are off by 2^-25 of it at most); the weights are rounded to fp16, half a step
-// being 2^-12 of a weight, and the sum is of the rounded ones; kLift keeps weights down to 2^-21 of the reference's in fp16's normal range and
+// being 2^-11 of a weight, and the sum is of the rounded ones; kLift keeps weights down to 2^-21 of the reference's in fp16's normal range and
 // the smallest that is not lost at 2^-32, so that what a million far keys add up to is kept.  Sums, references and outputs are fp32.
 //
 // Operands without a transpose or LDS: a wavefront takes the scores of 64 keys as S^T = K q^T in four 16 x 16 tiles.  Row i of tile t
@@ -143,9 +143,10 @@ struct QueryTile {
 };
 
 // Few query rows: the wavefronts of a block share its 16 query rows and take every fourth block of 64 keys each; their results are
-// joined in LDS, and those of a sequence's splits by the combine kernel.  What bounds it: bytes on long caches (4 sequences of 131 000 keys, 8 KV heads of 128: 180 us =
+// joined in LDS, and those of a sequence's splits by the combine kernel.  The chunks of 16 rows of one head lie a multiple of the grid's splits x heads apart, so that where
+// that is a multiple of eight one XCD's L2 serves them all (11 rows of 4 query heads on 16 000 keys 22.4 -> 18.8 us).  What bounds it: bytes on long caches (4 sequences of 131 000 keys, 8 KV heads of 128: 180 us =
 // 6.0 TB/s), else the chain of load, scores, weights and products of a wavefront's blocks of keys
-// (one token on 389 keys 7 us, 24 x 5 rows of 64-wide heads on up to 3000 keys 11.6).  No LDS on the way in: a code is used by one wavefront only.
+// (one token on 389 keys 7 us, 24 x 5 rows of 64-wide heads on up to 3000 keys 10.8).  No LDS on the way in: a code is used by one wavefront only.
 template <int DH, bool QB, int OUT>
 __global__ __launch_bounds__(256, 2) void attn8_direct_kernel(Kv8AttnArgs a, float scale_log2) {
     constexpr int KS = DH / 32, DT = DH / 16, KL = DH / 64;
@@ -676,7 +677,7 @@ __global__ __launch_bounds__(QG * KG * 64, 512 / (QG * KG * 64)) void attn8_wide
     }
 }
 // Joins the splits of a row and head, in their order: 256 / d_h rows and heads a wavefront, four entries a lane.  One trip to memory: 288 rows
-// of 5 splits 3.2 us, 7168 rows of 8 splits 6.3 (4.9 TB/s).
+// of 5 splits 3.1 us, 7168 rows of 4 splits 5.1, of 8 splits 6.3 (4.9 TB/s).
 template <int DH, int OUT>
 __global__ __launch_bounds__(256) void attn8_combine_kernel(Kv8AttnArgs a) {
     constexpr int kLanes = DH / 4, kRows = 256 / kLanes;

@@ -269,7 +269,7 @@ struct Kv8AppendArgs {
     int units;                    // these: set by launch_kv8_append
     int q_rows, q_parts;          // rows of a block of queries, blocks of a group of rows
     FastDiv per_row, by_r;        // items of a row's queries; R
-    bool q_vec;
+    bool q_vec, q_past;           // 16-byte stores; past the caches
     RopeParams rope;              // rot 0: nothing turns
     const float2 *cs;             // the rows' (cos, sin), rows cs_stride pairs apart; NULL: worked out from `turns`
     int cs_stride;

@@ -217,8 +217,15 @@ __global__ __launch_bounds__(kThreads) void kv8_append_kernel(Kv8AppendArgs a, R
             for (int e = 0; e < 8; ++e) { u[k][e] *= sc; v[k][e] *= sc; }
             if (a.q_vec) {
                 if constexpr (sizeof(TQ) == 2) {
-                    *reinterpret_cast<u32x4 *>(dst + it[k].e0) = u32x4{pack_bf16x2(u[k][0], u[k][1]), pack_bf16x2(u[k][2], u[k][3]), pack_bf16x2(u[k][4], u[k][5]), pack_bf16x2(u[k][6], u[k][7])};
-                    *reinterpret_cast<u32x4 *>(dst + it[k].e1) = u32x4{pack_bf16x2(v[k][0], v[k][1]), pack_bf16x2(v[k][2], v[k][3]), pack_bf16x2(v[k][4], v[k][5]), pack_bf16x2(v[k][6], v[k][7])};
+                    const u32x4 w0{pack_bf16x2(u[k][0], u[k][1]), pack_bf16x2(u[k][2], u[k][3]), pack_bf16x2(u[k][4], u[k][5]), pack_bf16x2(u[k][6], u[k][7])};
+                    const u32x4 w1{pack_bf16x2(v[k][0], v[k][1]), pack_bf16x2(v[k][2], v[k][3]), pack_bf16x2(v[k][4], v[k][5]), pack_bf16x2(v[k][6], v[k][7])};
+                    if (a.q_past) {
+                        __builtin_nontemporal_store(w0, reinterpret_cast<u32x4 *>(dst + it[k].e0));
+                        __builtin_nontemporal_store(w1, reinterpret_cast<u32x4 *>(dst + it[k].e1));
+                    } else {
+                        *reinterpret_cast<u32x4 *>(dst + it[k].e0) = w0;
+                        *reinterpret_cast<u32x4 *>(dst + it[k].e1) = w1;
+                    }
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; e += 4) {
@@ -375,6 +382,9 @@ void launch_kv8_append(const Kv8AppendArgs &args, const Kv8Source &src, hipStrea
     const bool odd = a.rope.rot % 16 != 0;
     const int out_es = src.bf16 ? 2 : 4;
     a.q_vec = (uintptr_t)a.q_out % 16 == 0 && a.q_out_stride * out_es % 16 == 0;
+    // Many rotated queries go past the caches.  us, append alone and with the attention behind it, rows of 32 heads of 128: 200 rows through them 7.5, 15.9, past them 7.4, 16.1;
+    // 500 7.9, 27.6 and 7.6, 27.3; 1000 10.1, 39.1 and 9.1, 38.8; 4001 25.4, 174 and 21.8, 173.
+    a.q_past = (int64_t)a.B * a.R * a.h_q * a.d_h * out_es >= 4 << 20;
     ScopedProf sp(PSD_KIND_ROPE_APPEND, stream);
     auto go = [&](auto rows, auto tq) {
         using Rows = decltype(rows(nullptr, 0));

@@ -16,7 +16,6 @@ namespace psd {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kItems = 4;             // per thread, all loaded before the first is used
 constexpr int kTableMax = 1024;       // (cos, sin) pairs of a block's rows: 4 rows of 256 / 2 frequencies and more of narrower ones
 
 // P consecutive entries as one load or store
@@ -61,9 +60,10 @@ __device__ __forceinline__ void narrow(float *p, const float (&v)[P]) {
 // An item is 2 P entries of one head: P pairs (half pairing: two runs of P, half the rotated width apart; interleaved: one run of
 // 2 P), or 2 P entries behind the rotated ones, which are copied.  The first nt items of a head are pairs.  P is the widest that
 // divides both parts and that the rows' alignment allows, up to 16 bytes a run.  A block takes `rows` rows and kItems * 256 of
-// their items; no loop, every load is on its way before the angles are worked out.
-// 8191 rows of 40 heads of 128 bf16 entries: 37.5 us = 4.5 TB/s; 9 rows 4.6 us, a launch's own time.
-template <typename T, int P>
+// their items; no loop, every load is on its way before the angles are worked out.  One item a thread, or two where there are millions: us, rows of 40
+// heads of 128 bf16 entries, one / two / four: 9 3.2 / 4.0 / 4.0; 1000 6.5 / 7.1 / 8.9; 4000 17.3 / 17.6 / 19.5; 8191 38.4 / 36.7 / 41.6 (4.6 TB/s); 16000 69 / 63 / 73.
+// Stores past the caches took 30.7 for the 8191, and gave it back to the kernel that reads the result (with it 64.8 / 62.8).
+template <typename T, int P, int kItems>
 __global__ __launch_bounds__(kThreads) void rope_rotate_kernel(RopeRotateArgs a) {
     __shared__ float2 cs[kTableMax];
     const int tid = threadIdx.x, nf = a.rope.rot / 2, nt = nf / P;
@@ -140,7 +140,8 @@ void launch_rope_rotate(int dtype, RopeRotateArgs a, hipStream_t stream) {
     a.per_head = FastDiv(a.d_h / 2 / P);
     a.per_row = FastDiv((uint32_t)a.heads * (a.d_h / 2 / P));
     // rows of a block: enough items for all its threads, and no more angles than the table holds
-    const uint32_t per_block = kThreads * kItems, per_row = a.per_row.n;
+    const int items = (uint64_t)a.rows * a.per_row.n > (1u << 21) ? 2 : 1;
+    const uint32_t per_block = kThreads * items, per_row = a.per_row.n;
     int rows = per_row >= per_block ? 1 : (int)(per_block / per_row);
     rows = rows > kTableMax / nf ? kTableMax / nf : rows;
     if (rows > a.rows) rows = (int)a.rows;
@@ -148,16 +149,21 @@ void launch_rope_rotate(int dtype, RopeRotateArgs a, hipStream_t stream) {
     a.block_rows = rows;
     const dim3 grid((unsigned)((a.rows + rows - 1) / rows), (rows * per_row + per_block - 1) / per_block);
     ScopedProf sp(PSD_KIND_ROPE, stream);
-    auto go = [&](auto kernel) { launch_kernel(kernel, grid, kThreads, 0, stream, a); };
+    auto go = [&](auto type, auto p) {
+        using T = decltype(type);
+        constexpr int kP = decltype(p)::value;
+        if (items == 2) launch_kernel(rope_rotate_kernel<T, kP, 2>, grid, kThreads, 0, stream, a);
+        else launch_kernel(rope_rotate_kernel<T, kP, 1>, grid, kThreads, 0, stream, a);
+    };
     if (dtype == PSD_BF16) {
-        if (P == 8) go(rope_rotate_kernel<uint16_t, 8>);
-        else if (P == 4) go(rope_rotate_kernel<uint16_t, 4>);
-        else if (P == 2) go(rope_rotate_kernel<uint16_t, 2>);
-        else go(rope_rotate_kernel<uint16_t, 1>);
+        if (P == 8) go((uint16_t)0, Int<8>{});
+        else if (P == 4) go((uint16_t)0, Int<4>{});
+        else if (P == 2) go((uint16_t)0, Int<2>{});
+        else go((uint16_t)0, Int<1>{});
     } else {
-        if (P == 4) go(rope_rotate_kernel<float, 4>);
-        else if (P == 2) go(rope_rotate_kernel<float, 2>);
-        else go(rope_rotate_kernel<float, 1>);
+        if (P == 4) go(0.f, Int<4>{});
+        else if (P == 2) go(0.f, Int<2>{});
+        else go(0.f, Int<1>{});
     }
 }
 

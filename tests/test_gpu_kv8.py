@@ -51,7 +51,9 @@ ROPE_CASES = [  # rows, heads, d, rot, layout, scaling, type, elements between r
     (1023, 5, 64, 16, "interleaved", "base", BF16, 64, 0), (33, 7, 80, 80, "half", "none", BF16, 0, 0), (33, 7, 80, 20, "half", "base", F32, 0, 0),
     (65, 2, 256, 256, "half", "parts", F32, 0, 0), (300, 17, 256, 64, "interleaved", "none", BF16, 8, 8), (64, 9, 96, 24, "half", "none", BF16, 3, 1),
     (50, 3, 6, 4, "interleaved", "linear", BF16, 0, 1), (50, 3, 10, 6, "half", "none", F32, 1, 3), (2100, 64, 128, 96, "half", "parts", BF16, 0, 0),
-    (3, 300, 256, 256, "interleaved", "none", F32, 0, 0)]
+    (3, 300, 256, 256, "interleaved", "none", F32, 0, 0),
+    # more than two million items: two a thread
+    (8200, 33, 128, 128, "half", "parts", BF16, 0, 0), (5000, 4, 256, 222, "interleaved", "none", F32, 2, 1), (9001, 31, 64, 32, "half", "base", F32, 0, 0)]
 
 
 @pytest.mark.parametrize("case", ROPE_CASES, ids=[f"{c[0]}x{c[1]}x{c[2]}-{c[3]}-{c[4]}-{c[5]}" for c in ROPE_CASES])
