@@ -152,7 +152,7 @@ __device__ __forceinline__ uint32_t shrink4(uint32_t w, float ratio) {
 // One launch, blocks of two kinds.  The first `units` blocks: the new tokens of one cache block of one KV head, K or V.  Thread t has the
 // items t and t + 256 of 64 rows x d / 16: their entries stay in registers from the one read, through the block's maximum, to
 // the codes.  The others rotate the query heads of up to 16 rows, 512 items, by angles that the block works out once for all heads.
-// What bounds it: bytes for prompts (4001 rows of 32 query and 8 KV heads of 128, bf16: 23 us = 3.9 TB/s), the chain load -> maximum -> scale -> store for
+// What bounds it: bytes for prompts (4001 rows of 32 query and 8 KV heads of 128, bf16: 22.8 us = 4.0 TB/s), the chain load -> maximum -> scale -> store for
 // few rows (9 rows, 32 and 32 heads: 5.5 us; 64 sequences of one row, 32 and 8: 7.4).  Why 64 rows of a KV head to a block: a scale's
 // tokens meet in one block, so no maximum crosses blocks, and a unit's 16 KB fit the registers.
 template <typename Rows, typename TQ, bool ODD>

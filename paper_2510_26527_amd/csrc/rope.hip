@@ -61,7 +61,7 @@ __device__ __forceinline__ void narrow(float *p, const float (&v)[P]) {
 // 2 P), or 2 P entries behind the rotated ones, which are copied.  The first nt items of a head are pairs.  P is the widest that
 // divides both parts and that the rows' alignment allows, up to 16 bytes a run.  A block takes `rows` rows and kItems * 256 of
 // their items; no loop, every load is on its way before the angles are worked out.  One item a thread, or two where there are millions: us, rows of 40
-// heads of 128 bf16 entries, one / two / four: 9 3.2 / 4.0 / 4.0; 1000 6.5 / 7.1 / 8.9; 4000 17.3 / 17.6 / 19.5; 8191 38.4 / 36.7 / 41.6 (4.6 TB/s); 16000 69 / 63 / 73.
+// heads of 128 bf16 entries, one / two / four: 9 3.2 / 4.0 / 4.0; 1000 6.5 / 7.1 / 8.9; 4000 17.3 / 17.6 / 19.5; 8191 38.4 / 36.7 / 41.6 (in a trace 33.1 = 5.07 TB/s); 16000 69 / 63 / 73.
 // Stores past the caches took 30.7 for the 8191, and gave it back to the kernel that reads the result (with it 64.8 / 62.8).
 template <typename T, int P, int kItems>
 __global__ __launch_bounds__(kThreads) void rope_rotate_kernel(RopeRotateArgs a) {
