@@ -226,7 +226,8 @@ psd_status psd_kv8_append(const psd_kv8_view *cache, const psd_rope *rope, const
  *   scale     0: 1 / sqrt(d_head)
  *   workspace 256-byte aligned, psd_kv8_attention_workspace_bytes() of the same numbers (0: none needed, or the call refuses them)
  * Scales in the cache must be positive, finite and between 2^-40 and 2^40.  What lies at positions that a row does not
- * see has no part in its result, whatever it is.  Sums, softmax and outputs in fp32, weights rounded to fp16. */
+ * see has no part in its result, whatever it is.  Softmax and sums in fp32; weights are rounded to fp16, and so are entries of a query
+ * below 2^-17 of its largest. */
 size_t psd_kv8_attention_workspace_bytes(int32_t batch, int32_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t d_head,
                                          int32_t len_upper_bound);
 psd_status psd_kv8_attention(const psd_kv8_view *cache, const void *q, void *out, int32_t n_new, int32_t n_q_heads, float scale,
