@@ -740,18 +740,28 @@ static int direct_range(long heads, int blocks) {
     const int nearest = (blocks + 2 * s.most) / (4 * s.most) * 4, range = nearest < 4 ? 4 : nearest;
     return (blocks + range - 1) / range <= s.cus ? range : ((blocks + s.most - 1) / s.most + 3) / 4 * 4;
 }
-// Wide kernel: as many as there are CUs for, and twice that where each still walks 12 blocks, three blocks at least to a split.  us: 64 heads
+// Wide kernel: as many as there are CUs for, and twice that where each wavefront still walks 12 blocks (24 in blocks of 64 rows), three blocks at least to a split.  us: 64 heads
 // (16 x 16 rows x 7 query heads), 65 blocks 2: 53.6, 4: 35.9, 8: 36.6; 126 blocks 4: 53.3, 8: 51.6; 48 heads (24 x 5 x 8), 47 blocks 2: 27, 5: 17.1, 10: 18.5; 8 heads (9 rows x 4), 16 blocks 1: 25.5,
 // 5: 13.7, 16: 15.5; 251 blocks 16: 32.8, 32: 28.4; 128 (4 x 33 rows x 32 heads), 17 blocks 1: 27.7, 2: 21.4, 4: 22.3; 64 blocks 2: 49.3, 4: 43.6.
-static int wide_splits(long heads, int blocks) {
+static int wide_splits(long heads, int blocks, int rows) {
     long splits = 256 / heads;
-    if (splits > 0 && blocks / splits >= 24) splits = 512 / heads;
+    if (splits > 0 && blocks / splits >= (rows == 64 ? 48 : 24)) splits = 512 / heads;
     const int most = blocks / 3;
     splits = splits < most ? splits : most;
     return splits < 1 ? 1 : (int)splits;
 }
 static long grid_heads(int B, int h_kv, int NQ, int rows) { return (long)B * h_kv * ((NQ + rows - 1) / rows); }
-static int wide_rows(int NQ) { return NQ > 64 ? 128 : 64; }
+// Rows of a block of the wide kernel.  A wavefront of the blocks of 64 rows walks every other block of keys, so that a step's work lies in twice as many
+// blocks of half the length: more CUs have some, and few long rows wait for less.  64 while those are all resident, but for short
+// chunks that fill the CUs already, and for long caches, where splits fill them.  us, 128 / 64 rows, by blocks of 128 rows x blocks of keys: 80 x 3 14.1 / 13.7, 104 x 4 14.8 / 14.0, 110 x 7
+// 18.1 / 12.7, 132 x 9 25.7 / 21.1, 160 x 5 20.7 / 17.7, 176 x 22 41.1 / 36.8, 176 x 68 87.7 / 84.7, 250 x 16 33.6 / 20.9, 256 x 8 28.4 / 23.1, 256 x 40 69.3 / 60.1, in chunks of 200 rows
+// 256 x 10 22.9 / 25.5; 128 x 28 37.9 / 33.0, 128 x 36 43.6 / 38.0, 128 x 51 46.7 / 50.1, 80 x 34 32.8 / 34.4, 96 x 134 73.5 / 93.4.
+static int wide_rows(int B, int h_kv, int NQ, int blocks) {
+    const long by_64 = grid_heads(B, h_kv, NQ, 64), by_128 = grid_heads(B, h_kv, NQ, 128);
+    if (NQ <= 64) return 64;
+    if (by_64 > 512 || (by_128 > 192 && NQ <= 512)) return 128;
+    return by_128 > 128 || 10l * blocks <= 3 * by_128 ? 64 : 128;
+}
 
 // Query rows of a block.  16, the direct kernel's, while all its blocks are resident and few keys are walked again for every 16 rows: it
 // begins and ends sooner (no barrier, no LDS on the way in).  Above, the wide kernel turns codes once for 32 rows and reads them from LDS; up
@@ -769,19 +779,23 @@ int kv8_attn_max_splits(int B, int R, int h_q, int h_kv, int d_h, int len_bound)
     const long heads = grid_heads(B, h_kv, NQ, 16);
     const DirectSplits s = direct_splits(heads, blocks);
     const int rounded = s.most + s.most / 2 + 1, d = rounded < s.cus ? rounded : s.cus;          // (six blocks a split become four)
-    const int w = NQ > 16 ? wide_splits(grid_heads(B, h_kv, NQ, wide_rows(NQ)), blocks) : 1;
-    return d > w ? d : w;
+    int most = d;
+    for (int rows = 64; rows <= 128 && NQ > 16; rows += 64) {
+        const int w = wide_splits(grid_heads(B, h_kv, NQ, rows), blocks, rows);
+        most = w > most ? w : most;
+    }
+    return most;
 }
 
 Kv8AttnPlan kv8_attn_plan(int B, int R, int h_q, int h_kv, int d_h, int len_bound) {
     const int NQ = h_q / h_kv * R, blocks = (len_bound + kKv8Block - 1) / kKv8Block;
     const int seen = (len_bound - R / 2 + kKv8Block - 1) / kKv8Block;                      // rows see half of the step's own keys on average
     Kv8AttnPlan p;
-    p.rows = direct(B, h_kv, NQ, d_h, seen) ? 16 : wide_rows(NQ);
+    p.rows = direct(B, h_kv, NQ, d_h, seen) ? 16 : wide_rows(B, h_kv, NQ, seen);
     if (p.rows == 16)
         p.range = direct_range(grid_heads(B, h_kv, NQ, 16), blocks);
     else {
-        const int splits = wide_splits(grid_heads(B, h_kv, NQ, p.rows), seen);
+        const int splits = wide_splits(grid_heads(B, h_kv, NQ, p.rows), seen, p.rows);
         p.range = (blocks + splits - 1) / splits;
     }
     p.splits = (blocks + p.range - 1) / p.range;

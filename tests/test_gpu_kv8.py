@@ -239,7 +239,7 @@ def test_append_never_writes_behind_the_cache():
 
 # ---------------------------------------------------------------------------------------------------- attention
 def _attention_oracle(c, q, lens, R, scale):
-    """q [B, R, h_q, d] fp64 -> the result and the weighted sum of |v|."""
+    """q [B, R, h_q, d] fp64 -> the result and the weighted sum of |v|, in it 2^-18 of the plain sum (see _room)."""
     B, _, h_q, d = q.shape
     out, room = np.zeros_like(q), np.zeros_like(q)
     for b in range(B):
@@ -251,13 +251,15 @@ def _attention_oracle(c, q, lens, R, scale):
                 s = k[:n] @ q[b, r, h] * scale
                 w = np.exp(s - s.max())
                 w /= w.sum()
-                out[b, r, h], room[b, r, h] = w @ v[:n], w @ np.abs(v[:n])
+                out[b, r, h], room[b, r, h] = w @ v[:n], w @ np.abs(v[:n]) + 2.0 ** -18 * np.abs(v[:n]).sum(0)
     return out, room
 
 
 def _room(ref, weighted):
-    """bf16's half step of the result; each weight rounded to fp16 (2^-11 of it, the smallest below 2^-34 of the largest); and for
-    scores, references and sums in fp32 a quarter of that again."""
+    """bf16's half step of the result; each weight rounded to fp16, 2^-11 of it; and for scores, references and sums in fp32 a quarter of
+    that again.  A weight below fp16's normal range is off by half of its smallest step, 2^-25, instead: weights are held times 2^7 against a
+    reference whose own weight is one of them, and times V's scale over the outputs' unit, 2^-3 at least, so that is 2^-25 / 2^7 * 2^3 = 2^-29
+    of |v| for a sum of weights of at least one, wherever the heavy keys' entries are zero: 2^-11 times the 2^-18 that `weighted` holds."""
     return np.abs(ref) * 2.0 ** -8 + weighted * (2.0 ** -11 + 2.0 ** -13)
 
 
@@ -269,7 +271,7 @@ ATTN_CASES = [  # B, R, h_q, h_kv, d, lens (before the rows)
     (3, 250, 12, 6, 64, [0, 100, 37]), (2, 170, 32, 16, 128, [70, 3]), (1, 100, 16, 4, 128, [4000]), (9, 12, 32, 8, 128, [2000 - 61 * i for i in range(9)]),
     (17, 20, 16, 16, 128, [3 * i for i in range(17)]), (6, 40, 32, 32, 64, [1200, 0, 64, 63, 1199, 500]), (1, 300, 3, 1, 128, [0]), (1, 2, 16, 1, 64, [129]), (9, 17, 2, 1, 64, [7 * i for i in range(9)]),
     (1, 100, 32, 8, 128, [4000]), (9, 12, 32, 8, 128, [4000 - 61 * i for i in range(9)]), (1, 11, 16, 4, 128, [8100]), (1, 1, 8, 2, 128, [17000]),
-    (5, 5, 16, 8, 64, [0, 900, 777, 1000, 63])]
+    (5, 5, 16, 8, 64, [0, 900, 777, 1000, 63]), (3, 130, 64, 64, 64, [0, 73, 5]), (5, 70, 64, 64, 128, [90, 0, 1, 63, 64])]
 
 
 @pytest.mark.parametrize("case", ATTN_CASES, ids=[f"{c[0]}x{c[1]}-{c[2]}/{c[3]}x{c[4]}-{max(c[5])}" for c in ATTN_CASES])
@@ -293,7 +295,7 @@ def test_attention(case):
 
 
 @pytest.mark.parametrize("R,h_kv,group,d", [(1, 1, 4, 128), (5, 1, 4, 128), (40, 1, 4, 128), (150, 1, 4, 64),
-                                            (150, 8, 4, 128), (20, 130, 1, 64), (20, 130, 1, 128)])        # the last three: blocks of 128 and of 64 rows
+                                            (150, 8, 4, 128), (20, 130, 1, 64), (20, 130, 1, 128), (150, 90, 1, 64), (150, 90, 1, 128)])        # the last five: blocks of 64 and of 128 rows
 def test_what_a_row_does_not_see_has_no_part_in_it(R, h_kv, group, d):
     """Later rows of the step, and everything behind it, may hold NaN; a row that sees one gets NaN in V's entries, or all over for K."""
     lens, B = [70, 200], 2
@@ -337,7 +339,7 @@ def test_attention_scores_far_apart_and_scales_far_apart():
         assert np.all(np.abs(got.double().cpu().numpy() - ref) <= _room(ref, weighted))
 
 
-@pytest.mark.parametrize("heads,R", [(1, 3), (2, 40), (5, 60), (64, 140)])            # the last: blocks of 128 rows
+@pytest.mark.parametrize("heads,R", [(1, 3), (2, 40), (5, 60), (64, 140), (256, 140)])            # the last two: blocks of 64 and of 128 rows
 @pytest.mark.parametrize("d", [64, 128])
 def test_attention_of_large_scores(heads, R, d):
     """Scores of 2^20 and 2^100, all equal or far apart: weights of 1 and 0."""
@@ -500,15 +502,16 @@ def test_forwards_on_an_8_bit_cache(shape, pack, w4):
     model.close()
 
 
-def test_a_long_prompt_on_an_8_bit_cache():
-    """More rows than the direct kernel takes: the wide kernel's fp16 output, for the tiled projections."""
-    shape, B = synth.Shape(1, 256, 8, 4, 64, 256, 128, 1.0e4), 2
+@pytest.mark.parametrize("h_q,h_kv,R", [(8, 4, 620), (32, 32, 560)])
+def test_a_long_prompt_on_an_8_bit_cache(h_q, h_kv, R):
+    """More rows than the direct kernel takes: the wide kernel's fp16 output, for the tiled projections, from blocks of 64 and of 128 rows."""
+    shape, B = synth.Shape(1, 256, h_q, h_kv, 64, 256, 128, 1.0e4), 2
     model = runtime.Model(shape, synth.make_weights(shape, 2, BF16, std=0.05)).pack()
     w, cfg = {k: v.cpu() for k, v in model.weights.items()}, ofwd.ModelConfig(**shape.asdict())
     kv = runtime.KVCache8(model, B, 704, fill_garbage=True)
     okv = Following(cfg, B, 704, kv)
     toks = synth.make_tokens(shape.vocab, (B, 660), 4)
-    for n in (620, 40):
+    for n in (R, 40):
         t = toks[:, int(okv.lens[0]):int(okv.lens[0]) + n]
         got = runtime.forward(model, kv, torch.from_numpy(t).cuda())
         _logits_close(got, ofwd.forward(cfg, w, t, okv), f"{n} rows")

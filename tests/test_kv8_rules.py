@@ -46,10 +46,11 @@ def test_splits_cover_the_keys_and_stay_within_what_workspaces_are_sized_for(rul
 
 @pytest.mark.parametrize("rows,B,R,h_q,h_kv,d,n", [
     (16, 1, 1, 32, 8, 128, 5000), (16, 1, 9, 32, 8, 128, 4009), (16, 1, 200, 2, 2, 64, 200),
-    (128, 3, 250, 12, 6, 64, 350), (128, 2, 170, 32, 16, 128, 240), (16, 1, 100, 16, 4, 128, 4100), (128, 1, 100, 32, 8, 128, 4100), (16, 9, 12, 32, 8, 128, 2012), (64, 9, 12, 32, 8, 128, 4012), (64, 5, 3, 416, 52, 64, 65),
+    (64, 3, 250, 12, 6, 64, 350), (64, 2, 170, 32, 16, 128, 240), (128, 3, 130, 64, 64, 64, 203), (128, 5, 70, 64, 64, 128, 160), (128, 2, 150, 90, 90, 128, 448),
+    (128, 1, 140, 256, 1, 64, 320), (128, 2, 560, 32, 32, 64, 560), (16, 1, 100, 16, 4, 128, 4100), (128, 1, 100, 32, 8, 128, 4100), (16, 9, 12, 32, 8, 128, 2012), (64, 9, 12, 32, 8, 128, 4012), (64, 5, 3, 416, 52, 64, 65),
     (16, 4, 5, 32, 8, 128, 16005), (64, 4, 5, 32, 8, 128, 32005),
-    (64, 17, 20, 16, 16, 128, 68), (64, 6, 40, 32, 32, 64, 1240), (128, 2, 150, 32, 8, 128, 448), (64, 2, 20, 130, 130, 64, 448),
-    (128, 1, 140, 64, 1, 64, 320), (16, 1, 9, 32, 8, 128, 17009), (64, 1, 9, 32, 8, 128, 25009), (128, 2, 620, 8, 4, 64, 620), (128, 1, 2001, 32, 32, 128, 2001)])
+    (64, 17, 20, 16, 16, 128, 68), (64, 6, 40, 32, 32, 64, 1240), (64, 2, 150, 32, 8, 128, 448), (64, 2, 20, 130, 130, 64, 448),
+    (64, 1, 140, 64, 1, 64, 320), (16, 1, 9, 32, 8, 128, 17009), (64, 1, 9, 32, 8, 128, 25009), (64, 2, 620, 8, 4, 64, 620), (128, 1, 2001, 32, 32, 128, 2001)])
 def test_which_kernel_takes_which_rows(rules, rows, B, R, h_q, h_kv, d, n):
     """Among them the shapes with which the GPU tests mean to reach the blocks of 64 and of 128 rows."""
     assert rules[0](B, R, h_q, h_kv, d, n).rows == rows
